@@ -153,6 +153,88 @@ int dr_spmm_bwd_adaptive(const dr_csr* At, const uint8_t* edge_class, const floa
                          const dr_degree_classes* cls, float* dXr, int accumulate, void* stream);
 
 /*
+ * Activation checkpoints in 8 bits: what a forward pass leaves for the backward pass, at a byte an element.
+ * A checkpoint of X[n,D] is q[n,D] (int8) and one scale byte b per group of DR_ACT8_GROUP consecutive columns of a row
+ * (the last group of a row may be narrower); it stands for q * 2^(b - 127).  b is the least one, and at least 1, with
+ * max|x| < 127.5 * 2^(b - 127) over the group, and q = x / 2^(b - 127) rounded to nearest, ties to even: a value is off by
+ * at most 2^(b - 128), no more than max|x| / 127.5 (2^-127 where b is 1).  b is at most 248: magnitudes above 127 * 2^121 are
+ * held as that.  A group that holds an infinity or a not-a-number has b = 255 and q = 0 and stands for not-a-numbers.
+ * Scales are powers of two, so that packing has one rounding and the value is exact in fp32 (and in bf16).
+ * scale: dr_act8_scale_bytes(n, D) bytes, 8-byte aligned; the byte of (row, group) is at
+ * ((row / 8) * groups + group) * 8 + row % 8, and bytes of rows past n are written as 0.
+ * A width of D = k holds the values of a CBSR.  1 <= D <= DR_MAX_D, n < 2^31.
+ */
+#define DR_ACT8_GROUP 32
+typedef struct dr_act8 {
+    int8_t*  q;
+    uint8_t* scale;
+} dr_act8;
+size_t dr_act8_scale_bytes(int64_t n, int32_t D);
+int dr_act8_pack(const float* X, int64_t n, int32_t D, const dr_act8* out, void* stream);
+int dr_act8_unpack(const dr_act8* in, int64_t n, int32_t D, float* X, void* stream);
+
+/*
+ * Weight gradient of a dense projection Z = A W whose input A[n,D] was kept as a checkpoint:
+ *     dW[D,F] (=|+=) A^T dZ,          A the values the checkpoint stands for, dZ[n,F] in fp32.
+ * accumulate == 0 overwrites dW.  Products are exact to 2^-24 and summed in fp32 and fp64, in a fixed order.
+ * 1 <= D, F <= DR_MAX_D.  workspace: at least dr_act8_wgrad_workspace_bytes() bytes, 256-byte aligned, contents undefined
+ * before and after; it belongs to one call at a time.
+ */
+size_t dr_act8_wgrad_workspace_bytes(int64_t n, int32_t D, int32_t F);
+int dr_act8_wgrad(const dr_act8* A, int64_t n, int32_t D, const float* dZ, int32_t F, float* dW, int accumulate,
+                  void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Residual block around a layer: the norm behind the layer, its gate and residual scale, the residual sum and the norm in
+ * front of the next layer, in one pass over the rows of one node type.
+ *     X_out = X + scale * sigmoid(G) * (norm(Y) * w_after + b_after)        (Y[n,D]: the layer's output)
+ *     N     = norm(X_out) * w_before + b_before                             (the next layer's input)
+ *     norm(x) = x * r,  r = 1 / sqrt(mean(x^2) + eps)                 DR_ROWNORM_RMS
+ *     norm(x) = (x - m) * r,  m = mean(x), r = 1 / sqrt(mean((x - m)^2) + eps)      DR_ROWNORM_LAYER
+ * Means are over the D entries of a row.  G has gate_cols columns: D (a gate per element), 1 (one per row) or 0 (no gate,
+ * G NULL).  w_*, b_* and scale are [D]; NULL stands for ones, zeros and ones.
+ * Y NULL: only the norm in front, N of X (X_out, G, y and g are NULL then, and saved.x is the checkpoint of X).
+ * N NULL: only the part behind the layer.  One of Y and N is given.
+ */
+#define DR_ROWNORM_RMS   0
+#define DR_ROWNORM_LAYER 1
+typedef struct dr_block {
+    int32_t norm;                 /* DR_ROWNORM_*, of both norms */
+    int32_t gate_cols;            /* 0, 1 or D */
+    float eps;                    /* > 0 */
+    const float *w_after, *b_after, *scale, *w_before, *b_before;
+} dr_block;
+/* What the forward pass leaves for the backward pass; every part may be NULL in the forward pass and is not kept then.
+ * Statistics are [n] (r) for DR_ROWNORM_RMS and [n,2] (m, r) for DR_ROWNORM_LAYER.  Checkpoints of X_out, Y and G (only where
+ * gate_cols is D): q NULL = not kept. */
+typedef struct dr_block_saved {
+    float *stats_after, *stats_before;
+    dr_act8 x, y, g;
+} dr_block_saved;
+/* X_out and N may be X, Y or G themselves, at the same address: every row is read before it is written. */
+int dr_block_fwd(const dr_block* block, int64_t n, int32_t D, const float* X, const float* Y, const float* G, float* X_out,
+                 float* N, const dr_block_saved* saved, void* stream);
+
+/*
+ * Backward.  dX_out, dN: gradients of X_out and N (NULL: zero; a NULL dN leaves out the norm in front).  X_out, Y and G come as
+ * fp32 tensors or, where those are NULL, from the checkpoints in `saved`; not both.  Y and saved.y both absent: only the norm in
+ * front.  The statistics are the saved ones, so that with checkpoints the gradient is the formula's at the values that the
+ * checkpoints stand for, with the statistics of the exact rows.
+ * dX[n,D] (of the residual input; without Y, of the norm's input), dY[n,D], dG[n,gate_cols] and the sums over rows dw_after, db_after, dscale,
+ * dw_before, db_before [D] are overwritten; NULL = not wanted.  dX and dY may be dX_out, dN or a given Y, X_out or G themselves.
+ * workspace: at least dr_block_bwd_workspace_bytes() bytes, 256-byte aligned, contents undefined before and after; it
+ * belongs to one call at a time.  Sums over rows have a fixed order: a pass is reproducible bit for bit.
+ */
+typedef struct dr_block_grads {
+    float *dX, *dY, *dG;
+    float *dw_after, *db_after, *dscale, *dw_before, *db_before;
+} dr_block_grads;
+size_t dr_block_bwd_workspace_bytes(int64_t n, int32_t D);
+int dr_block_bwd(const dr_block* block, int64_t n, int32_t D, const float* dX_out, const float* dN, const float* X_out, const float* Y,
+                 const float* G, const dr_block_saved* saved, const dr_block_grads* grads, void* workspace,
+                 size_t workspace_bytes, void* stream);
+
+/*
  * Setup: stable CSR transpose (Alg. 2 stage 1, "transpose A to CSC").  Row j of the result lists the
  * entries of column j of A in increasing original row and, for equal rows, original storage order.
  * Outputs t_rowptr[n_cols+1], t_colidx[nnz], t_vals[nnz] (t_vals and A->vals may both be NULL for a

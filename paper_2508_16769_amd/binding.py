@@ -23,6 +23,9 @@ DR_ERR_HIP = -3
 DR_ERR_WORKSPACE = -4
 DR_NORM_MEAN = 0
 DR_NORM_SYM = 1
+DR_ROWNORM_RMS = 0
+DR_ROWNORM_LAYER = 1
+DR_ACT8_GROUP = 32
 DR_OVERLAP_AUTO = 0
 DR_OVERLAP_ON = 1
 DR_OVERLAP_OFF = 2
@@ -32,6 +35,8 @@ EXPORTS = (
     "dr_last_error", "dr_abi_version", "dr_topk", "dr_spmm_fwd", "dr_spmm_bwd",
     "dr_spmm_plan_create", "dr_spmm_plan_info", "dr_spmm_bwd_planned", "dr_spmm_plan_destroy",
     "dr_topk_ranked", "dr_spmm_fwd_adaptive", "dr_degree_edge_classes", "dr_spmm_bwd_adaptive",
+    "dr_act8_scale_bytes", "dr_act8_pack", "dr_act8_unpack", "dr_act8_wgrad_workspace_bytes", "dr_act8_wgrad",
+    "dr_block_fwd", "dr_block_bwd_workspace_bytes", "dr_block_bwd",
     "dr_csr_transpose_workspace_bytes", "dr_csr_transpose",
     "dr_csr_normalize_workspace_bytes", "dr_csr_normalize", "dr_csr_normalize_noalloc",
     "heteroconv_create", "heteroconv_create_per_relation", "heteroconv_get_k", "heteroconv_profile_k", "heteroconv_fwd", "heteroconv_bwd", "heteroconv_get_transpose", "heteroconv_destroy",
@@ -94,10 +99,44 @@ def load() -> ctypes.CDLL:
         lib.dr_last_error.restype = ctypes.c_char_p
         lib.dr_csr_transpose_workspace_bytes.restype = ctypes.c_size_t
         lib.dr_csr_normalize_workspace_bytes.restype = ctypes.c_size_t
+        _declare_row_operators(lib)
         lib.heteroconv_kernel_name.restype = ctypes.c_char_p
         lib.hgnn_num_params.restype = ctypes.c_int64
         _lib = lib
     return _lib
+
+
+class dr_act8(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
+
+
+class dr_block(ctypes.Structure):
+    _fields_ = [("norm", ctypes.c_int32), ("gate_cols", ctypes.c_int32), ("eps", ctypes.c_float)] + [
+        (n, ctypes.c_void_p) for n in ("w_after", "b_after", "scale", "w_before", "b_before")]
+
+
+class dr_block_saved(ctypes.Structure):
+    _fields_ = [("stats_after", ctypes.c_void_p), ("stats_before", ctypes.c_void_p), ("x", dr_act8), ("y", dr_act8), ("g", dr_act8)]
+
+
+class dr_block_grads(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("dX", "dY", "dG", "dw_after", "db_after", "dscale", "dw_before", "db_before")]
+
+
+def _declare_row_operators(lib) -> None:
+    """Argument types of the row operators, so that their calls pass plain integers (a call of these takes microseconds)."""
+    p, i64, i32, size = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_size_t
+    for name, res, args in (
+            ("dr_act8_scale_bytes", size, (i64, i32)),
+            ("dr_act8_pack", i32, (p, i64, i32, p, p)),
+            ("dr_act8_unpack", i32, (p, i64, i32, p, p)),
+            ("dr_act8_wgrad_workspace_bytes", size, (i64, i32, i32)),
+            ("dr_act8_wgrad", i32, (p, i64, i32, p, i32, p, i32, p, size, p)),
+            ("dr_block_fwd", i32, (p, i64, i32, p, p, p, p, p, p, p)),
+            ("dr_block_bwd_workspace_bytes", size, (i64, i32)),
+            ("dr_block_bwd", i32, (p, i64, i32, p, p, p, p, p, p, p, p, size, p))):
+        f = getattr(lib, name)
+        f.restype, f.argtypes = res, args
 
 
 def _check(rc: int) -> None:
@@ -226,6 +265,85 @@ def dr_spmm_bwd_adaptive(At: Csr, edge_class: torch.Tensor, dH: torch.Tensor, xr
     a, c = At.c(), dr_degree_classes(*[int(v) for v in classes])
     _check(load().dr_spmm_bwd_adaptive(ctypes.byref(a), _ptr(edge_class), _ptr(dH), _ptr(xr_idx), ctypes.c_int32(D),
                                        ctypes.byref(c), _ptr(dXr), ctypes.c_int(1 if accumulate else 0), _stream(stream)))
+
+
+def _address(t) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def _act8(ckpt) -> dr_act8:
+    """A checkpoint is a pair of tensors (q [n, D] int8, scale bytes)."""
+    return dr_act8() if ckpt is None else dr_act8(ckpt[0].data_ptr(), ckpt[1].data_ptr())
+
+
+def _stream_of(stream) -> int:
+    if stream is None:
+        stream = torch.cuda.current_stream()
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def dr_act8_scale_bytes(n: int, D: int) -> int:
+    return load().dr_act8_scale_bytes(n, D)
+
+
+def alloc_act8(n: int, D: int, device="cuda"):
+    """Room for a checkpoint of a matrix [n, D]: (q, scale)."""
+    return (torch.empty((n, D), dtype=torch.int8, device=device),
+            torch.empty(dr_act8_scale_bytes(n, D), dtype=torch.uint8, device=device))
+
+
+def dr_act8_pack(X: torch.Tensor, ckpt, stream=None) -> None:
+    n, D = X.shape
+    _check(load().dr_act8_pack(X.data_ptr(), n, D, ctypes.byref(_act8(ckpt)), _stream_of(stream)))
+
+
+def dr_act8_unpack(ckpt, X: torch.Tensor, stream=None) -> None:
+    n, D = X.shape
+    _check(load().dr_act8_unpack(ctypes.byref(_act8(ckpt)), n, D, X.data_ptr(), _stream_of(stream)))
+
+
+def dr_act8_wgrad_workspace_bytes(n: int, D: int, F: int) -> int:
+    return load().dr_act8_wgrad_workspace_bytes(n, D, F)
+
+
+def dr_act8_wgrad(ckpt, dZ: torch.Tensor, dW: torch.Tensor, workspace: torch.Tensor, accumulate: bool = False, stream=None) -> None:
+    n, D = ckpt[0].shape
+    _check(load().dr_act8_wgrad(ctypes.byref(_act8(ckpt)), n, D, dZ.data_ptr(), dZ.shape[1], dW.data_ptr(), 1 if accumulate else 0,
+                                workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_of(stream)))
+
+
+def _gate_cols(G, g8) -> int:
+    return G.shape[1] if G is not None else 0 if g8 is None else g8[0].shape[1]
+
+
+def dr_block_fwd(X: torch.Tensor, Y: Optional[torch.Tensor], G: Optional[torch.Tensor], X_out: Optional[torch.Tensor],
+                 N: Optional[torch.Tensor], norm: int = DR_ROWNORM_RMS, eps: float = 1e-5, w_after=None, b_after=None, scale=None,
+                 w_before=None, b_before=None, stats_after=None, stats_before=None, x8=None, y8=None, g8=None, stream=None) -> None:
+    """x8, y8, g8: room for checkpoints of X_out, Y and G (pairs (q, scale)), or None."""
+    n, D = X.shape
+    b = dr_block(norm, _gate_cols(G, g8), eps, _address(w_after), _address(b_after), _address(scale), _address(w_before), _address(b_before))
+    s = dr_block_saved(_address(stats_after), _address(stats_before), _act8(x8), _act8(y8), _act8(g8))
+    _check(load().dr_block_fwd(ctypes.byref(b), n, D, X.data_ptr(), _address(Y), _address(G), _address(X_out), _address(N),
+                               ctypes.byref(s), _stream_of(stream)))
+
+
+def dr_block_bwd_workspace_bytes(n: int, D: int) -> int:
+    return load().dr_block_bwd_workspace_bytes(n, D)
+
+
+def dr_block_bwd(dX_out: Optional[torch.Tensor], dN: Optional[torch.Tensor], X_out: Optional[torch.Tensor], Y: Optional[torch.Tensor],
+                 G: Optional[torch.Tensor], norm: int = DR_ROWNORM_RMS, eps: float = 1e-5, w_after=None, b_after=None, scale=None,
+                 w_before=None, b_before=None, stats_after=None, stats_before=None, x8=None, y8=None, g8=None, dX=None, dY=None,
+                 dG=None, dw_after=None, db_after=None, dscale=None, dw_before=None, db_before=None, workspace=None, stream=None) -> None:
+    """x8, y8, g8: checkpoints that stand in for X_out, Y and G where those are None."""
+    n, D = (dX_out if dX_out is not None else dN).shape
+    b = dr_block(norm, _gate_cols(G, g8), eps, _address(w_after), _address(b_after), _address(scale), _address(w_before), _address(b_before))
+    s = dr_block_saved(_address(stats_after), _address(stats_before), _act8(x8), _act8(y8), _act8(g8))
+    g = dr_block_grads(_address(dX), _address(dY), _address(dG), _address(dw_after), _address(db_after), _address(dscale),
+                       _address(dw_before), _address(db_before))
+    wsb = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(load().dr_block_bwd(ctypes.byref(b), n, D, _address(dX_out), _address(dN), _address(X_out), _address(Y), _address(G),
+                               ctypes.byref(s), ctypes.byref(g), _address(workspace), wsb, _stream_of(stream)))
 
 
 def dr_csr_transpose_workspace_bytes(n_rows: int, n_cols: int, nnz: int) -> int:

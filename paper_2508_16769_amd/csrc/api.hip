@@ -1,5 +1,5 @@
 // C ABI entry points: host-side argument validation, then the kernel launchers.
-#include "dr_internal.h"
+#include "act8.h"
 
 #include <cstring>
 
@@ -144,6 +144,143 @@ int dr_spmm_bwd_adaptive(const dr_csr* At, const uint8_t* edge_class, const floa
     DRC_REQUIRE(At->n_cols < (int64_t(1) << 30), "dr_spmm_bwd_adaptive: 2^30 or more destinations");
     DRC_REQUIRE(At->n_cols * (int64_t)D < (int64_t(1) << 32), "dr_spmm_bwd_adaptive: M*D >= 2^32");
     return launch_spmm_bwd_adaptive(At, edge_class, dH, xr_idx, D, cls, dXr, accumulate, as_stream(stream));
+}
+
+static int check_rows(int64_t n, int32_t D, const char* fn) {
+    DRC_REQUIRE(n >= 0, "%s: negative row count", fn);
+    DRC_REQUIRE(n < (int64_t(1) << 31), "%s: more than 2^31-1 rows", fn);
+    DRC_REQUIRE(D >= 1, "%s: D must be >= 1 (got %d)", fn, D);
+    if (D > DR_MAX_D) return fail(DR_ERR_UNSUPPORTED, "%s: D = %d exceeds DR_MAX_D = %d", fn, D, DR_MAX_D);
+    return DR_OK;
+}
+
+static int check_act8(const dr_act8* c, const char* fn, const char* name) {
+    DRC_REQUIRE(c != nullptr && c->q != nullptr && c->scale != nullptr, "%s: null checkpoint (%s)", fn, name);
+    DRC_REQUIRE(aligned(c->scale, 8), "%s: scales of checkpoint %s must be 8-byte aligned", fn, name);
+    return DR_OK;
+}
+
+static int check_workspace(const void* ws, size_t have, size_t need, const char* fn) {
+    DRC_REQUIRE(ws != nullptr, "%s: null workspace", fn);
+    DRC_REQUIRE(aligned(ws, 256), "%s: workspace must be 256-byte aligned", fn);
+    if (have < need) return fail(DR_ERR_WORKSPACE, "%s: workspace has %zu bytes, needs %zu", fn, have, need);
+    return DR_OK;
+}
+
+size_t dr_act8_scale_bytes(int64_t n, int32_t D) {
+    if (n < 0 || D < 1) return 0;
+    return (size_t)((n + 7) / 8) * act_groups(D) * 8;
+}
+
+int dr_act8_pack(const float* X, int64_t n, int32_t D, const dr_act8* out, void* stream) {
+    DRC_TRY(check_rows(n, D, "dr_act8_pack"));
+    if (n == 0) return DR_OK;
+    DRC_REQUIRE(X != nullptr, "dr_act8_pack: null pointer");
+    DRC_REQUIRE(aligned(X, 4), "dr_act8_pack: misaligned pointer");
+    DRC_TRY(check_act8(out, "dr_act8_pack", "out"));
+    return launch_act8_pack(X, n, D, *out, as_stream(stream));
+}
+
+int dr_act8_unpack(const dr_act8* in, int64_t n, int32_t D, float* X, void* stream) {
+    DRC_TRY(check_rows(n, D, "dr_act8_unpack"));
+    if (n == 0) return DR_OK;
+    DRC_REQUIRE(X != nullptr, "dr_act8_unpack: null pointer");
+    DRC_REQUIRE(aligned(X, 4), "dr_act8_unpack: misaligned pointer");
+    DRC_TRY(check_act8(in, "dr_act8_unpack", "in"));
+    return launch_act8_unpack(*in, n, D, X, as_stream(stream));
+}
+
+size_t dr_act8_wgrad_workspace_bytes(int64_t n, int32_t D, int32_t F) {
+    if (n < 0 || D < 1 || F < 1) return 0;
+    return act8_wgrad_workspace(n, D, F);
+}
+
+int dr_act8_wgrad(const dr_act8* A, int64_t n, int32_t D, const float* dZ, int32_t F, float* dW, int accumulate, void* workspace,
+                  size_t workspace_bytes, void* stream) {
+    DRC_TRY(check_rows(n, D, "dr_act8_wgrad"));
+    DRC_REQUIRE(F >= 1, "dr_act8_wgrad: F must be >= 1 (got %d)", F);
+    if (F > DR_MAX_D) return fail(DR_ERR_UNSUPPORTED, "dr_act8_wgrad: F = %d exceeds DR_MAX_D = %d", F, DR_MAX_D);
+    DRC_REQUIRE(dW != nullptr, "dr_act8_wgrad: null dW");
+    if (n > 0) {
+        DRC_TRY(check_act8(A, "dr_act8_wgrad", "A"));
+        DRC_REQUIRE(dZ != nullptr, "dr_act8_wgrad: null dZ");
+    }
+    DRC_REQUIRE(aligned(dZ, 4) && aligned(dW, 4), "dr_act8_wgrad: misaligned pointer");
+    DRC_TRY(check_workspace(workspace, workspace_bytes, act8_wgrad_workspace(n, D, F), "dr_act8_wgrad"));
+    return launch_act8_wgrad(n > 0 ? *A : dr_act8{}, n, D, dZ, F, dW, accumulate != 0, workspace, as_stream(stream));
+}
+
+static int check_block(const dr_block* b, int32_t D, const char* fn) {
+    DRC_REQUIRE(b != nullptr, "%s: null block", fn);
+    DRC_REQUIRE(b->norm == DR_ROWNORM_RMS || b->norm == DR_ROWNORM_LAYER, "%s: unknown norm %d", fn, b->norm);
+    DRC_REQUIRE(b->eps > 0.0f && b->eps < 1e30f, "%s: eps must be positive", fn);
+    DRC_REQUIRE(b->gate_cols == 0 || b->gate_cols == 1 || b->gate_cols == D, "%s: gate_cols = %d is not 0, 1 or D = %d", fn, b->gate_cols, D);
+    DRC_REQUIRE(aligned(b->w_after, 4) && aligned(b->b_after, 4) && aligned(b->scale, 4) && aligned(b->w_before, 4) && aligned(b->b_before, 4),
+                "%s: misaligned parameter vector", fn);
+    return DR_OK;
+}
+
+int dr_block_fwd(const dr_block* block, int64_t n, int32_t D, const float* X, const float* Y, const float* G, float* X_out, float* N,
+                 const dr_block_saved* saved, void* stream) {
+    DRC_TRY(check_rows(n, D, "dr_block_fwd"));
+    DRC_TRY(check_block(block, D, "dr_block_fwd"));
+    if (n == 0) return DR_OK;
+    const dr_block_saved S = saved ? *saved : dr_block_saved{};
+    DRC_REQUIRE(X != nullptr, "dr_block_fwd: null X");
+    DRC_REQUIRE(Y != nullptr || N != nullptr, "dr_block_fwd: neither Y nor N");
+    DRC_REQUIRE((Y != nullptr) == (X_out != nullptr), "dr_block_fwd: Y and X_out must both be given or both be NULL");
+    DRC_REQUIRE((G != nullptr) == (block->gate_cols != 0), "dr_block_fwd: G and gate_cols = %d do not match", block->gate_cols);
+    DRC_REQUIRE(Y != nullptr || (G == nullptr && S.y.q == nullptr && S.g.q == nullptr && S.stats_after == nullptr),
+                "dr_block_fwd: a gate, statistics or checkpoints of a layer's output without Y");
+    DRC_REQUIRE(N != nullptr || S.stats_before == nullptr, "dr_block_fwd: statistics of a norm in front without N");
+    DRC_REQUIRE(S.g.q == nullptr || block->gate_cols == D, "dr_block_fwd: a checkpoint of G needs gate_cols = D");
+    DRC_REQUIRE(X_out == nullptr || X_out != N, "dr_block_fwd: X_out and N are the same");
+    DRC_REQUIRE(aligned(X, 4) && aligned(Y, 4) && aligned(G, 4) && aligned(X_out, 4) && aligned(N, 4) && aligned(S.stats_after, 4) &&
+                    aligned(S.stats_before, 4),
+                "dr_block_fwd: misaligned pointer");
+    if (S.x.q) DRC_TRY(check_act8(&S.x, "dr_block_fwd", "x"));
+    if (S.y.q) DRC_TRY(check_act8(&S.y, "dr_block_fwd", "y"));
+    if (S.g.q) DRC_TRY(check_act8(&S.g, "dr_block_fwd", "g"));
+    return launch_block_fwd(BlockFwd{*block, n, D, X, Y, G, X_out, N, S}, as_stream(stream));
+}
+
+size_t dr_block_bwd_workspace_bytes(int64_t n, int32_t D) {
+    if (n < 0 || D < 1) return 0;
+    return block_bwd_workspace(n, D);
+}
+
+int dr_block_bwd(const dr_block* block, int64_t n, int32_t D, const float* dX_out, const float* dN, const float* X_out, const float* Y,
+                 const float* G, const dr_block_saved* saved, const dr_block_grads* grads, void* workspace, size_t workspace_bytes,
+                 void* stream) {
+    DRC_TRY(check_rows(n, D, "dr_block_bwd"));
+    DRC_TRY(check_block(block, D, "dr_block_bwd"));
+    DRC_REQUIRE(grads != nullptr, "dr_block_bwd: null grads");
+    const dr_block_saved S = saved ? *saved : dr_block_saved{};
+    const dr_block_grads& g = *grads;
+    const bool after = Y != nullptr || S.y.q != nullptr, gated = G != nullptr || S.g.q != nullptr;
+    if (n > 0) {
+        DRC_REQUIRE(dX_out != nullptr || dN != nullptr, "dr_block_bwd: neither dX_out nor dN");
+        DRC_REQUIRE(Y == nullptr || S.y.q == nullptr, "dr_block_bwd: Y and its checkpoint are both given");
+        DRC_REQUIRE(G == nullptr || S.g.q == nullptr, "dr_block_bwd: G and its checkpoint are both given");
+        DRC_REQUIRE(X_out == nullptr || S.x.q == nullptr, "dr_block_bwd: X_out and its checkpoint are both given");
+        DRC_REQUIRE(dN == nullptr || X_out != nullptr || S.x.q != nullptr, "dr_block_bwd: dN without X_out or its checkpoint");
+        DRC_REQUIRE(dN == nullptr || S.stats_before != nullptr, "dr_block_bwd: dN without saved.stats_before");
+        DRC_REQUIRE(!after || S.stats_after != nullptr, "dr_block_bwd: Y without saved.stats_after");
+        DRC_REQUIRE(gated == (block->gate_cols != 0) && (after || !gated), "dr_block_bwd: G and gate_cols = %d do not match", block->gate_cols);
+        DRC_REQUIRE(S.g.q == nullptr || block->gate_cols == D, "dr_block_bwd: a checkpoint of G needs gate_cols = D");
+        DRC_REQUIRE(after || (!g.dY && !g.dG && !g.dw_after && !g.db_after && !g.dscale), "dr_block_bwd: gradients behind the layer without Y");
+        DRC_REQUIRE(gated || !g.dG, "dr_block_bwd: dG without G");
+        if (S.x.q) DRC_TRY(check_act8(&S.x, "dr_block_bwd", "x"));
+        if (S.y.q) DRC_TRY(check_act8(&S.y, "dr_block_bwd", "y"));
+        if (S.g.q) DRC_TRY(check_act8(&S.g, "dr_block_bwd", "g"));
+    }
+    DRC_REQUIRE(g.dX == nullptr || g.dX != g.dY, "dr_block_bwd: dX and dY are the same");
+    DRC_REQUIRE(aligned(dX_out, 4) && aligned(dN, 4) && aligned(X_out, 4) && aligned(Y, 4) && aligned(G, 4) && aligned(S.stats_after, 4) &&
+                    aligned(S.stats_before, 4) && aligned(g.dX, 4) && aligned(g.dY, 4) && aligned(g.dG, 4) && aligned(g.dw_after, 4) &&
+                    aligned(g.db_after, 4) && aligned(g.dscale, 4) && aligned(g.dw_before, 4) && aligned(g.db_before, 4),
+                "dr_block_bwd: misaligned pointer");
+    DRC_TRY(check_workspace(workspace, workspace_bytes, block_bwd_workspace(n, D), "dr_block_bwd"));
+    return launch_block_bwd(BlockBwd{*block, n, D, dX_out, dN, X_out, Y, G, S, g, nullptr, 0}, workspace, as_stream(stream));
 }
 
 size_t dr_csr_transpose_workspace_bytes(int64_t n_rows, int64_t n_cols, int64_t nnz) {
