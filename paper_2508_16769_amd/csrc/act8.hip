@@ -61,60 +61,318 @@ int launch_act8_unpack(const dr_act8& in, int64_t n, int D, float* X, hipStream_
 }
 
 // ---------------------------------------------------------------------------------------------------
-// dW[D,F] = A^T dZ.  A workgroup sums a 16 x 16 tile of dW over one span of rows; spans are added by a second kernel, in 64 bits
-// and a fixed order.
+// dW[D,F] = A^T dZ, the contraction running over the rows.
+//
+// Arithmetic.  What a code stands for, q * 2^s, is a bf16 number exactly; dZ is cut into three bf16 numbers, x = x1 + x2 + x3,
+// by taking the upper half of x, of x - x1 and of x - x1 - x2: 3 x 8 significant bits hold all 24.  Three exact bf16 products per
+// term then are the fp32 product (a projection whose input is held in fp32 needs six).  Leading products and small ones have
+// accumulators of their own, which start from zero every kFlush chunks and are added to the running sum with one rounding:
+// inside the matrix unit what lies below the running sum is cut off, always downwards, which over many rows adds up.
+//
+// Layout.  The 16x16x32 instruction takes eight consecutive contraction indices, rows, per lane: a unit is eight rows of one
+// column, 16 bytes.  A thread loads its column's eight rows (64 neighbouring columns per wavefront and row) and puts whole units
+// into LDS, so nothing is transposed.  The scales of a unit's eight rows lie side by side: one load.  Rows past the end and columns
+// past the widths read as zero through the buffer descriptors.
+//
+// Pipeline.  Eight wavefronts, LDS doubled, one barrier per chunk of rows; half of the wavefronts stage the next chunk before they
+// multiply, the other half after, so that vector and matrix instructions of a SIMD's two wavefronts overlap.  A workgroup takes one tile of
+// dW and every S-th chunk; partial sums go to the workspace and are added by a second kernel, in 64 bits and a fixed order.
 // ---------------------------------------------------------------------------------------------------
-constexpr int kWgTile = 16;
-static int wgrad_spans(int64_t n) {
-    const int64_t s = (n + 2047) / 2048;
-    return (int)(s < 1 ? 1 : (s > 256 ? 256 : s));
-}
-size_t act8_wgrad_workspace(int64_t n, int D, int F) { return sizeof(float) * (size_t)wgrad_spans(n) * D * F; }
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+using Buf = __amdgpu_buffer_rsrc_t;
 
-__global__ __launch_bounds__(kWgTile* kWgTile) void act8_wgrad_kernel(const int8_t* __restrict__ q, const uint8_t* __restrict__ scale, int64_t n, int D,
-                                                                      int groups, const float* __restrict__ dZ, int F, int64_t span,
-                                                                      float* __restrict__ part) {
-    __shared__ float a[kWgTile][kWgTile + 1], b[kWgTile][kWgTile + 1];
-    const int x = threadIdx.x % kWgTile, y = threadIdx.x / kWgTile;
-    const int d = blockIdx.x * kWgTile + x, f = blockIdx.y * kWgTile + x;
-    const int64_t end = min(n, (int64_t)(blockIdx.z + 1) * span);
-    float acc = 0.f;
-    for (int64_t r0 = (int64_t)blockIdx.z * span; r0 < end; r0 += kWgTile) {
-        const int64_t row = r0 + y;
-        const bool on = row < end;
-        a[y][x] = on && d < D ? (float)q[(size_t)row * D + d] * act_factor(scale[act_scale_at(row, d / kActGroup, groups)]) : 0.f;
-        b[y][x] = on && f < F ? dZ[(size_t)row * F + f] : 0.f;
-        __syncthreads();
-        float sum = 0.f;
+constexpr int kGradWaves = 8, kGradThreads = 64 * kGradWaves;
+constexpr int kFlush = 4;                          // chunks that the matrix unit sums up by itself
+constexpr int kGradWgs = 256;                      // one workgroup per compute unit
+constexpr int kOutside = 0x40000000;               // an offset outside every chunk
+
+// TD x TF entries of dW; WA x WB wavefronts side by side on them, WK groups of those on 32 rows of a chunk each
+template <int TD_, int TF_, int WA_, int WB_> struct GradTile {
+    static constexpr int TD = TD_, TF = TF_, WA = WA_, WB = WB_, WK = kGradWaves / (WA * WB);
+    static constexpr int CR = 32 * WK, RG = CR / 8;             // rows and units per column of a chunk
+    static constexpr int AU = RG * TD, BU = RG * TF;            // units of A and of one part of dZ
+    static constexpr int BUF = AU + 3 * BU;
+    static constexpr int MA = TD / (16 * WA), MB = TF / (16 * WB);      // 16 x 16 blocks per wavefront
+    static_assert(AU <= kGradThreads && BU <= kGradThreads && AU % 64 == 0 && BU % 64 == 0 && MA >= 1 && MB >= 1);
+};
+
+struct GradArgs {
+    const int8_t* q;
+    const uint8_t* scale;
+    const float* dZ;
+    float* part;
+    int64_t n;
+    int D, groups, F, tiles_f, splits;
+};
+
+__device__ __forceinline__ Buf chunk_view(const void* p, int64_t bytes) {
+    const uint64_t at = reinterpret_cast<uint64_t>(p);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32));
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((uint64_t)hi << 32 | lo), (short)0,
+                                             __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000);
+}
+// the upper halves of a and b as two bf16 numbers
+__device__ __forceinline__ uint32_t upper2(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+__device__ __forceinline__ uint32_t bits(float x) { return __builtin_bit_cast(uint32_t, x); }
+__device__ __forceinline__ float of_bits(uint32_t x) { return __builtin_bit_cast(float, x); }
+
+template <typename T> __device__ __forceinline__ void grad_walk_init(f32x4 (&c)[T::MA][T::MB]) {
 #pragma unroll
-        for (int k = 0; k < kWgTile; ++k) sum = fmaf(a[k][y], b[k][x], sum);
-        acc += sum;
-        __syncthreads();
-    }
-    const int dd = blockIdx.x * kWgTile + y;
-    if (dd < D && f < F) part[((size_t)blockIdx.z * D + dd) * F + f] = acc;
+    for (int i = 0; i < T::MA; ++i)
+#pragma unroll
+        for (int j = 0; j < T::MB; ++j) c[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 }
 
-__global__ __launch_bounds__(256) void act8_wgrad_sum_kernel(const float* __restrict__ part, int spans, int64_t count, int accumulate, float* dW) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= count) return;
-    double s = accumulate ? (double)dW[i] : 0.0;
-    for (int p = 0; p < spans; ++p) s += (double)part[(size_t)p * count + i];
-    dW[i] = (float)s;
+template <typename T> __global__ __launch_bounds__(kGradThreads, 2) void act8_wgrad_kernel(GradArgs a) {
+    extern __shared__ bf16x8 smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wk = wave / (T::WA * T::WB), wa = wave % (T::WA * T::WB) / T::WB, wb = wave % T::WB;
+    const int z = blockIdx.x % a.splits, tile = blockIdx.x / a.splits;
+    const int d0 = tile / a.tiles_f * T::TD, f0 = tile % a.tiles_f * T::TF;
+    const int ca = d0 + tid % T::TD, ra = tid / T::TD * 8;      // this thread's units: column and first row of A, of dZ
+    const int cb = f0 + tid % T::TF, rb = tid / T::TF * 8;
+    const bool has_a = wave * 64 < T::AU, has_b = wave * 64 < T::BU;    // whole wavefronts
+    const int D = a.D, F = a.F, G8 = a.groups * 8;
+    const int at_a = ca < D ? ra * D + ca : kOutside, at_b = cb < F ? (rb * F + cb) * 4 : kOutside;
+    const int at_s = ca < D ? (ra >> 3) * G8 + ca / kActGroup * 8 : kOutside;
+    const int chunks = (int)((a.n + T::CR - 1) / T::CR);
+
+    uint32_t code[8];
+    u32x2 scales;
+    float y[8];
+    auto load = [&](int chunk) {                                // past the last chunk: reads nothing
+        const int64_t base = (int64_t)chunk * T::CR;
+        const int64_t left = a.n > base ? (a.n - base < T::CR ? a.n - base : T::CR) : 0;
+        if (has_a) {
+            const Buf q = chunk_view(a.q + base * D, left * D), s = chunk_view(a.scale + base / 8 * G8, (left + 7) / 8 * G8);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) code[j] = __builtin_amdgcn_raw_buffer_load_b8(q, at_a + j * D, 0, 0);
+            scales = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(s, at_s, 0, 0));
+        }
+        if (has_b) {
+            const Buf b = chunk_view(a.dZ + base * F, left * F * 4);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = of_bits(__builtin_amdgcn_raw_buffer_load_b32(b, at_b + j * F * 4, 0, 0));
+        }
+    };
+    auto commit = [&](int chunk, int to) {
+        bf16x8* const buf = smem + to * T::BUF;
+        if (has_a) {
+            // bytes of rows past the end may hold anything: they are zeros here
+            const int64_t rows = a.n - ((int64_t)chunk * T::CR + ra);
+            if (rows < 8) {
+                const uint64_t keep = rows <= 0 ? 0 : (uint64_t(1) << (8 * rows)) - 1;
+                scales[0] &= (uint32_t)keep;
+                scales[1] &= (uint32_t)(keep >> 32);
+            }
+            uint32_t v[8], w[4];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                // 255 << 23 is an infinity and the codes of such a group are zeros: not-a-numbers
+                const float f = of_bits(((scales[j >> 2] >> (8 * (j & 3))) & 255u) << 23);
+                v[j] = bits((float)(int8_t)code[j] * f);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = upper2(v[2 * j], v[2 * j + 1]);
+            buf[tid] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
+        }
+        if (has_b) {
+            uint32_t x1[8], x2[8], x3[8];
+            float most = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                most = fmaxf(most, fabsf(y[j]));
+                x1[j] = bits(y[j]);
+                const float r = y[j] - of_bits(x1[j] & 0xffff0000u);
+                x2[j] = bits(r);
+                x3[j] = bits(r - of_bits(x2[j] & 0xffff0000u));
+            }
+            if (__builtin_amdgcn_ballot_w64(most == __builtin_inff())) {     // an infinity has no remainder
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (fabsf(y[j]) == __builtin_inff()) x2[j] = x3[j] = 0;
+            }
+            auto put = [&](int part, const uint32_t (&x)[8]) {
+                uint32_t w[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = upper2(x[2 * j], x[2 * j + 1]);
+                buf[T::AU + part * T::BU + tid] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
+            };
+            put(0, x1);
+            put(1, x2);
+            put(2, x3);
+        }
+    };
+
+    f32x4 acc[T::MA][T::MB], hi[T::MA][T::MB], lo[T::MA][T::MB];
+    grad_walk_init<T>(acc);
+    grad_walk_init<T>(hi);
+    grad_walk_init<T>(lo);
+    const auto flush = [&]() {
+#pragma unroll
+        for (int i = 0; i < T::MA; ++i)
+#pragma unroll
+            for (int j = 0; j < T::MB; ++j) {
+                acc[i][j] += hi[i][j] + lo[i][j];
+                hi[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+                lo[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+    };
+    const auto multiply = [&](int from) {
+        const bf16x8* const buf = smem + from * T::BUF;
+        const int rg = 4 * wk + (lane >> 4), col = lane & 15;
+        bf16x8 fa[T::MA];
+#pragma unroll
+        for (int i = 0; i < T::MA; ++i) fa[i] = buf[rg * T::TD + 16 * (wa * T::MA + i) + col];
+#pragma unroll
+        for (int j = 0; j < T::MB; ++j) {
+            bf16x8 fb[3];
+#pragma unroll
+            for (int p = 0; p < 3; ++p) fb[p] = buf[T::AU + p * T::BU + rg * T::TF + 16 * (wb * T::MB + j) + col];
+#pragma unroll
+            for (int i = 0; i < T::MA; ++i) lo[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[2], fa[i], lo[i][j], 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < T::MA; ++i) lo[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[1], fa[i], lo[i][j], 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < T::MA; ++i) hi[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[0], fa[i], hi[i][j], 0, 0, 0);
+        }
+    };
+    const auto walk = [&](bool first) {
+        int chunk = z, cur = 0, since = 0;
+        if (chunk < chunks) {
+            load(chunk);
+            commit(chunk, 0);
+            load(chunk + a.splits);
+        }
+        for (; chunk < chunks; chunk += a.splits, cur ^= 1) {
+            __syncthreads();                                    // this chunk is in LDS; the other buffer may be overwritten
+            const int next = chunk + a.splits;
+            if (first) {
+                commit(next, cur ^ 1);
+                load(next + a.splits);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(cur);
+            if (++since == kFlush) {
+                flush();
+                since = 0;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (!first) {
+                commit(next, cur ^ 1);
+                load(next + a.splits);
+            }
+        }
+        flush();
+    };
+    if (wave < kGradWaves / 2) walk(true);
+    else walk(false);
+    // lane: row 16 i + (lane & 15) of the wavefront's part of the tile, columns 16 j + 4 (lane >> 4) ..
+    float* const out = a.part + ((size_t)blockIdx.x * T::WK + wk) * T::TD * T::TF;
+#pragma unroll
+    for (int i = 0; i < T::MA; ++i)
+#pragma unroll
+        for (int j = 0; j < T::MB; ++j)
+            *reinterpret_cast<f32x4*>(out + (size_t)(16 * (wa * T::MA + i) + (lane & 15)) * T::TF + 16 * (wb * T::MB + j) + 4 * (lane >> 4)) = acc[i][j];
+}
+
+// dW = the sum over a tile's partials: wavefront w of the workgroup sums partials w, w + 16, ... of 64 x 4 consecutive entries, then
+// the 16 sums are added in order, in 64 bits (up to 1024 partials of nearly equal size lose as much in 32-bit sums as everything before).
+constexpr int kSumWaves = 16;
+__global__ __launch_bounds__(64 * kSumWaves) void act8_wgrad_sum_kernel(const float* __restrict__ part, int parts, int TD, int TF, int tiles_f, int D,
+                                                                        int F, int accumulate, float* dW) {
+    __shared__ f64x4 sums[kSumWaves][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int blocks = TD * TF / 256, tile = blockIdx.x / blocks;
+    const int at = blockIdx.x % blocks * 256 + 4 * lane;
+    const float* const src = part + (size_t)tile * parts * TD * TF + at;
+    f64x4 s = {0., 0., 0., 0.};
+    int b = wave;
+    for (; b + 3 * kSumWaves < parts; b += 4 * kSumWaves) {     // four loads in flight
+        f32x4 v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const f32x4*>(src + (size_t)(b + u * kSumWaves) * TD * TF);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) s += __builtin_convertvector(v[u], f64x4);
+    }
+    for (; b < parts; b += kSumWaves) s += __builtin_convertvector(*reinterpret_cast<const f32x4*>(src + (size_t)b * TD * TF), f64x4);
+    sums[wave][lane] = s;
+    __syncthreads();
+    if (wave != 0) return;
+    f64x4 t = sums[0][lane];
+#pragma unroll
+    for (int w = 1; w < kSumWaves; ++w) t += sums[w][lane];
+    const int d = tile / tiles_f * TD + at / TF, f = tile % tiles_f * TF + at % TF;
+    if (d >= D) return;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+        if (f + r < F) {
+            float* const o = dW + (size_t)d * F + f + r;
+            *o = (float)(accumulate ? (double)*o + t[r] : t[r]);
+        }
+}
+
+// Calls f(GradTile<...>{}): a tile as wide as the matrix, up to 128 either way.
+template <typename F> static int with_grad_tile(int D, int Fw, F f) {
+    if (D <= 32) {
+        if (Fw <= 32) return f(GradTile<32, 32, 2, 1>{});
+        if (Fw <= 64) return f(GradTile<32, 64, 2, 2>{});
+        return f(GradTile<32, 128, 2, 4>{});
+    }
+    if (D <= 64) {
+        if (Fw <= 32) return f(GradTile<64, 32, 2, 2>{});
+        if (Fw <= 64) return f(GradTile<64, 64, 2, 2>{});
+        return f(GradTile<64, 128, 2, 4>{});
+    }
+    if (Fw <= 32) return f(GradTile<128, 32, 4, 2>{});
+    if (Fw <= 64) return f(GradTile<128, 64, 4, 2>{});
+    return f(GradTile<128, 128, 2, 4>{});
+}
+// Workgroups per tile of dW: one per compute unit in all, a chunk each at least.
+template <typename T> static int grad_splits(int64_t n, int D, int F) {
+    const int64_t tiles = (int64_t)((D + T::TD - 1) / T::TD) * ((F + T::TF - 1) / T::TF), chunks = (n + T::CR - 1) / T::CR;
+    const int64_t most = tiles < kGradWgs ? kGradWgs / tiles : 1;
+    return (int)(chunks < 1 ? 1 : chunks < most ? chunks : most);
+}
+
+size_t act8_wgrad_workspace(int64_t n, int D, int F) {
+    size_t bytes = 0;
+    with_grad_tile(D, F, [&](auto tile) -> int {
+        using T = decltype(tile);
+        const size_t tiles = (size_t)((D + T::TD - 1) / T::TD) * ((F + T::TF - 1) / T::TF);
+        bytes = sizeof(float) * tiles * grad_splits<T>(n, D, F) * T::WK * T::TD * T::TF;
+        return DR_OK;
+    });
+    return bytes;
 }
 
 int launch_act8_wgrad(const dr_act8& A, int64_t n, int D, const float* dZ, int F, float* dW, bool accumulate, void* ws, hipStream_t s) {
-    const int spans = n == 0 ? 0 : wgrad_spans(n);
-    if (spans) {
-        const int64_t span = ((n + spans - 1) / spans + kWgTile - 1) / kWgTile * kWgTile;
-        hipLaunchKernelGGL(act8_wgrad_kernel, dim3((D + kWgTile - 1) / kWgTile, (F + kWgTile - 1) / kWgTile, spans), dim3(kWgTile * kWgTile), 0, s, A.q,
-                           A.scale, n, D, act_groups(D), dZ, F, span, static_cast<float*>(ws));
-    }
-    const int64_t count = (int64_t)D * F;
-    hipLaunchKernelGGL(act8_wgrad_sum_kernel, dim3((unsigned)((count + 255) / 256)), dim3(256), 0, s, static_cast<const float*>(ws), spans, count,
-                       accumulate ? 1 : 0, dW);
-    DRC_HIP(hipGetLastError());
-    return DR_OK;
+    return with_grad_tile(D, F, [&](auto tile) -> int {
+        using T = decltype(tile);
+        static PerDevice cache;
+        constexpr size_t lds = sizeof(bf16x8) * 2 * T::BUF;
+        int dev = 0, ready = 0;
+        DRC_HIP(hipGetDevice(&dev));
+        DRC_TRY(cache.get(dev, &ready, [&](int* r) -> int {
+            DRC_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&act8_wgrad_kernel<T>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+            *r = 1;
+            return DR_OK;
+        }));
+        const int tiles_d = (D + T::TD - 1) / T::TD, tiles_f = (F + T::TF - 1) / T::TF;
+        const int splits = n == 0 ? 0 : grad_splits<T>(n, D, F);
+        if (splits) {
+            const GradArgs a{A.q, A.scale, dZ, static_cast<float*>(ws), n, D, act_groups(D), F, tiles_f, splits};
+            hipLaunchKernelGGL((act8_wgrad_kernel<T>), dim3((unsigned)(tiles_d * tiles_f * splits)), dim3(kGradThreads), lds, s, a);
+        }
+        hipLaunchKernelGGL(act8_wgrad_sum_kernel, dim3((unsigned)(tiles_d * tiles_f * (T::TD * T::TF / 256))), dim3(64 * kSumWaves), 0, s,
+                           static_cast<const float*>(ws), splits * T::WK, T::TD, T::TF, tiles_f, D, F, accumulate ? 1 : 0, dW);
+        DRC_HIP(hipGetLastError());
+        return DR_OK;
+    });
 }
 
 }  // namespace drc
