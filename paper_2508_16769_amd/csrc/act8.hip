@@ -3,58 +3,54 @@
 
 namespace drc {
 
-constexpr int kPackThreads = 256;
-
 template <typename T>
-__global__ __launch_bounds__(kPackThreads) void act8_pack_kernel(const float* __restrict__ X, int64_t n, int D, int groups, int8_t* __restrict__ q,
-                                                                 uint8_t* __restrict__ scale) {
-    constexpr int R = kPackThreads / T::LPR;
-    const int t = threadIdx.x % T::LPR;
-    for (int64_t r0 = (int64_t)blockIdx.x * R; r0 < n; r0 += (int64_t)gridDim.x * R) {
-        const int64_t row = r0 + threadIdx.x / T::LPR;
-        const bool on = row < n;
+__global__ __launch_bounds__(kRowThreads) void act8_pack_kernel(const float* X, int64_t n, int D, int8_t* q, uint8_t* scale) {
+    const RowLane<T> l(D);
+    const int groups = act_groups(D);
+    const int64_t n8 = (n + 7) & ~int64_t(7);                   // the rows that fill up the last eight have scale bytes
+    for (int64_t r0 = (int64_t)blockIdx.x * T::R; r0 < n8; r0 += (int64_t)gridDim.x * T::R) {
+        const int left = (int)(n - r0 < T::R ? (n > r0 ? n - r0 : 0) : T::R);
+        uint32_t raw[T::E];
         float x[T::E];
-        row_load<T>(X + (size_t)row * D, t, D, on, x);
-        row_pack<T>(q, scale, row, n, t, D, groups, on, x);
+        load_rows<T>(rows_view(X, r0, left, 4 * D), l, raw);
+#pragma unroll
+        for (int i = 0; i < T::E; ++i) x[i] = of_bits(raw[i]);
+        store_codes<T>(rows_view(q, r0, left, D), scales_view(scale, r0, n, groups), l, l.row < left, x);
     }
 }
 
 template <typename T>
-__global__ __launch_bounds__(kPackThreads) void act8_unpack_kernel(const int8_t* __restrict__ q, const uint8_t* __restrict__ scale, int64_t n, int D,
-                                                                   int groups, float* __restrict__ X) {
-    constexpr int R = kPackThreads / T::LPR;
-    const int t = threadIdx.x % T::LPR;
-    for (int64_t r0 = (int64_t)blockIdx.x * R; r0 < n; r0 += (int64_t)gridDim.x * R) {
-        const int64_t row = r0 + threadIdx.x / T::LPR;
-        const bool on = row < n;
+__global__ __launch_bounds__(kRowThreads) void act8_unpack_kernel(const int8_t* q, const uint8_t* scale, int64_t n, int D, float* X) {
+    const RowLane<T> l(D);
+    const int groups = act_groups(D);
+    for (int64_t r0 = (int64_t)blockIdx.x * T::R; r0 < n; r0 += (int64_t)gridDim.x * T::R) {
+        const int left = (int)(n - r0 < T::R ? n - r0 : T::R);
+        uint32_t code[T::E], s[T::V];
         float x[T::E];
-        row_unpack<T>(q, scale, row, t, D, groups, on, x);
-        row_store<T>(X + (size_t)row * D, t, D, on, x);
+        load_codes<T>(rows_view(q, r0, left, D), scales_view(scale, r0, n, groups), l, code, s);
+        decode<T>(code, s, l.row < left, x);
+        store_rows<T>(rows_view(X, r0, left, 4 * D), l, x);
     }
 }
 
-static unsigned row_blocks(int64_t n, int rows_per_block, int64_t most) {
-    const int64_t b = (n + rows_per_block - 1) / rows_per_block;
+static unsigned row_blocks(int64_t rows, int rows_per_block, int64_t most) {
+    const int64_t b = (rows + rows_per_block - 1) / rows_per_block;
     return (unsigned)(b < most ? b : most);
 }
 
 int launch_act8_pack(const float* X, int64_t n, int D, const dr_act8& out, hipStream_t s) {
-    const bool vector = D % 4 == 0 && aligned(X, 16) && aligned(out.q, 4);
-    return with_row_tile(D, vector, [&](auto tile) -> int {
+    return with_row_tile(D, D % 4 == 0 && aligned(X, 16) && aligned(out.q, 4), [&](auto tile) -> int {
         using T = decltype(tile);
-        hipLaunchKernelGGL((act8_pack_kernel<T>), dim3(row_blocks(n, kPackThreads / T::LPR, 8192)), dim3(kPackThreads), 0, s, X, n, D, act_groups(D),
-                           out.q, out.scale);
+        hipLaunchKernelGGL((act8_pack_kernel<T>), dim3(row_blocks((n + 7) / 8 * 8, T::R, 8192)), dim3(kRowThreads), 0, s, X, n, D, out.q, out.scale);
         DRC_HIP(hipGetLastError());
         return DR_OK;
     });
 }
 
 int launch_act8_unpack(const dr_act8& in, int64_t n, int D, float* X, hipStream_t s) {
-    const bool vector = D % 4 == 0 && aligned(X, 16) && aligned(in.q, 4);
-    return with_row_tile(D, vector, [&](auto tile) -> int {
+    return with_row_tile(D, D % 4 == 0 && aligned(X, 16) && aligned(in.q, 4), [&](auto tile) -> int {
         using T = decltype(tile);
-        hipLaunchKernelGGL((act8_unpack_kernel<T>), dim3(row_blocks(n, kPackThreads / T::LPR, 8192)), dim3(kPackThreads), 0, s, in.q, in.scale, n, D,
-                           act_groups(D), X);
+        hipLaunchKernelGGL((act8_unpack_kernel<T>), dim3(row_blocks(n, T::R, 8192)), dim3(kRowThreads), 0, s, in.q, in.scale, n, D, X);
         DRC_HIP(hipGetLastError());
         return DR_OK;
     });
@@ -78,17 +74,12 @@ int launch_act8_unpack(const dr_act8& in, int64_t n, int D, float* X, hipStream_
 // multiply, the other half after, so that vector and matrix instructions of a SIMD's two wavefronts overlap.  A workgroup takes one tile of
 // dW and every S-th chunk; partial sums go to the workspace and are added by a second kernel, in 64 bits and a fixed order.
 // ---------------------------------------------------------------------------------------------------
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef double f64x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-using Buf = __amdgpu_buffer_rsrc_t;
 
 constexpr int kGradWaves = 8, kGradThreads = 64 * kGradWaves;
 constexpr int kFlush = 4;                          // chunks that the matrix unit sums up by itself
 constexpr int kGradWgs = 256;                      // one workgroup per compute unit
-constexpr int kOutside = 0x40000000;               // an offset outside every chunk
 
 // TD x TF entries of dW; WA x WB wavefronts side by side on them, WK groups of those on 32 rows of a chunk each
 template <int TD_, int TF_, int WA_, int WB_> struct GradTile {
@@ -109,16 +100,8 @@ struct GradArgs {
     int D, groups, F, tiles_f, splits;
 };
 
-__device__ __forceinline__ Buf chunk_view(const void* p, int64_t bytes) {
-    const uint64_t at = reinterpret_cast<uint64_t>(p);
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32));
-    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((uint64_t)hi << 32 | lo), (short)0,
-                                             __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000);
-}
 // the upper halves of a and b as two bf16 numbers
 __device__ __forceinline__ uint32_t upper2(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
-__device__ __forceinline__ uint32_t bits(float x) { return __builtin_bit_cast(uint32_t, x); }
-__device__ __forceinline__ float of_bits(uint32_t x) { return __builtin_bit_cast(float, x); }
 
 template <typename T> __device__ __forceinline__ void grad_walk_init(f32x4 (&c)[T::MA][T::MB]) {
 #pragma unroll
@@ -148,13 +131,13 @@ template <typename T> __global__ __launch_bounds__(kGradThreads, 2) void act8_wg
         const int64_t base = (int64_t)chunk * T::CR;
         const int64_t left = a.n > base ? (a.n - base < T::CR ? a.n - base : T::CR) : 0;
         if (has_a) {
-            const Buf q = chunk_view(a.q + base * D, left * D), s = chunk_view(a.scale + base / 8 * G8, (left + 7) / 8 * G8);
+            const Buf q = buf_view(a.q + base * D, left * D), s = buf_view(a.scale + base / 8 * G8, (left + 7) / 8 * G8);
 #pragma unroll
             for (int j = 0; j < 8; ++j) code[j] = __builtin_amdgcn_raw_buffer_load_b8(q, at_a + j * D, 0, 0);
             scales = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(s, at_s, 0, 0));
         }
         if (has_b) {
-            const Buf b = chunk_view(a.dZ + base * F, left * F * 4);
+            const Buf b = buf_view(a.dZ + base * F, left * F * 4);
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] = of_bits(__builtin_amdgcn_raw_buffer_load_b32(b, at_b + j * F * 4, 0, 0));
         }

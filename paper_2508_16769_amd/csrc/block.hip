@@ -14,234 +14,335 @@
 
 namespace drc {
 
-constexpr int kBlockThreads = 256;
 constexpr int kSums = 5;                       // dw_after, db_after, dscale, dw_before, db_before
 
-template <typename T> __device__ __forceinline__ void vec_load(const float* __restrict__ p, int t, int D, float none, float (&x)[T::E]) {
+// a parameter vector's elements of this lane; zeros past the width
+template <typename T> __device__ __forceinline__ void vec_load(const float* p, const RowLane<T>& l, int D, float none, float (&x)[T::E]) {
 #pragma unroll
     for (int v = 0; v < T::V; ++v)
 #pragma unroll
         for (int j = 0; j < T::W; ++j) {
-            const int c = tile_col<T>(t, v) + j;
+            const int c = l.col(v) + j;
             x[T::W * v + j] = c < D ? (p ? p[c] : none) : 0.f;
         }
 }
 
-// mean (0 for RMS) and reciprocal deviation of a row
-template <typename T> __device__ __forceinline__ void row_stats(const float (&x)[T::E], int t, int D, bool layer, float eps, float& m, float& r) {
-    const float inv = 1.0f / (float)D;
-    m = 0.f;
+// mean (0 for RMS) and reciprocal deviation of a row; elements past the width are zeros
+template <typename T>
+__device__ __forceinline__ void row_stats(const float (&x)[T::E], const RowLane<T>& l, RowSums& sums, int D, bool layer, float inv, float eps, float& m,
+                                          float& r) {
     float s = 0.f;
+    m = 0.f;
     if (layer) {
 #pragma unroll
         for (int i = 0; i < T::E; ++i) s += x[i];
-        m = lane_sum<T::LPR>(s) * inv;
+        m = sums.sum<T>(s) * inv;
         s = 0.f;
-    }
 #pragma unroll
-    for (int i = 0; i < T::E; ++i) {
-        const bool in = tile_col<T>(t, i / T::W) < D;
-        const float c = in ? x[i] - m : 0.f;
-        s = fmaf(c, c, s);
+        for (int i = 0; i < T::E; ++i) {
+            const float c = l.col(i / T::W) < D ? x[i] - m : 0.f;
+            s = fmaf(c, c, s);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < T::E; ++i) s = fmaf(x[i], x[i], s);
     }
-    r = 1.0f / sqrtf(lane_sum<T::LPR>(s) * inv + eps);
+    r = __builtin_amdgcn_rsqf(fmaf(sums.sum<T>(s), inv, eps));       // (off by an ulp at most)
 }
-__device__ __forceinline__ void put_stats(float* p, int64_t row, bool layer, float m, float r) {
-    if (layer) { p[2 * row] = m; p[2 * row + 1] = r; }
-    else p[row] = r;
-}
-__device__ __forceinline__ void get_stats(const float* p, int64_t row, bool layer, float& m, float& r) {
-    m = layer ? p[2 * row] : 0.f;
-    r = layer ? p[2 * row + 1] : p[row];
-}
-__device__ __forceinline__ float sigmoid(float g) { return 1.0f / (1.0f + expf(-g)); }
+__device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.0f + expf(-g)); }
 
-template <typename T> __global__ __launch_bounds__(kBlockThreads) void block_fwd_kernel(BlockFwd a) {
-    constexpr int R = kBlockThreads / T::LPR;
-    const int t = threadIdx.x % T::LPR, D = a.D, groups = act_groups(D);
-    const bool layer = a.b.norm == DR_ROWNORM_LAYER;
+// Statistics are [n] or [n,2]: one load or store either way.
+__device__ __forceinline__ Buf stats_view(const float* p, int64_t r0, int left, bool layer) { return rows_view(p, r0, left, layer ? 8 : 4); }
+__device__ __forceinline__ void load_stats(Buf b, int row, bool layer, float& m, float& r) {
+    if (layer) {
+        const u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(b, row * 8, 0, 0));
+        m = of_bits(v[0]);
+        r = of_bits(v[1]);
+    } else {
+        m = 0.f;
+        r = of_bits(__builtin_amdgcn_raw_buffer_load_b32(b, row * 4, 0, 0));
+    }
+}
+__device__ __forceinline__ void store_stats(Buf b, int row, bool first, bool layer, float m, float r) {
+    if (layer) __builtin_amdgcn_raw_buffer_store_b64(u32x2{bits(m), bits(r)}, b, first ? row * 8 : kOutside, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b32(bits(r), b, first ? row * 4 : kOutside, 0, 0);
+}
+
+template <typename T> __device__ __forceinline__ void fill(uint32_t (&x)[T::E], uint32_t v) {
+#pragma unroll
+    for (int i = 0; i < T::E; ++i) x[i] = v;
+}
+
+// What a row brings, as it comes from memory: loaded a block of rows ahead.
+template <typename T, bool GATED> struct FwdRow { uint32_t x[T::E], y[T::E], g[GATED ? T::E : 1]; };
+
+// CKPT: checkpoints are kept (of any of the three tensors).
+template <typename T, bool GATED, bool CKPT> __global__ __launch_bounds__(kRowThreads) void block_fwd_kernel(BlockFwd a) {
+    __shared__ float sh[2][kRowThreads / kWave][2];
+    RowSums sums{sh, 0};
+    const int D = a.D, groups = act_groups(D);
+    const RowLane<T> l(D);
+    const bool layer = a.b.norm == DR_ROWNORM_LAYER, full = a.b.gate_cols == D;
+    const float inv = 1.0f / (float)D, eps = a.b.eps;
     float wa[T::E], ba[T::E], sc[T::E], wb[T::E], bb[T::E];
-    vec_load<T>(a.b.w_after, t, D, 1.f, wa);
-    vec_load<T>(a.b.b_after, t, D, 0.f, ba);
-    vec_load<T>(a.b.scale, t, D, 1.f, sc);
-    vec_load<T>(a.b.w_before, t, D, 1.f, wb);
-    vec_load<T>(a.b.b_before, t, D, 0.f, bb);
-    for (int64_t r0 = (int64_t)blockIdx.x * R; r0 < a.n; r0 += (int64_t)gridDim.x * R) {
-        const int64_t row = r0 + threadIdx.x / T::LPR;
-        const bool on = row < a.n;
-        const size_t at = (size_t)row * D;
-        float x[T::E];
-        row_load<T>(a.X + at, t, D, on, x);
+    vec_load<T>(a.b.w_after, l, D, 1.f, wa);
+    vec_load<T>(a.b.b_after, l, D, 0.f, ba);
+    vec_load<T>(a.b.scale, l, D, 1.f, sc);
+    vec_load<T>(a.b.w_before, l, D, 1.f, wb);
+    vec_load<T>(a.b.b_before, l, D, 0.f, bb);
+    const int64_t end = CKPT ? (a.n + 7) & ~int64_t(7) : a.n, step = (int64_t)gridDim.x * T::R;
+    const auto left_of = [&](int64_t r0) { return (int)(a.n - r0 < T::R ? (a.n > r0 ? a.n - r0 : 0) : T::R); };
+    FwdRow<T, GATED> raw;
+    const auto load = [&](int64_t r0) {
+        const int left = left_of(r0);
+        load_rows<T>(rows_view(a.X, r0, left, 4 * D), l, raw.x);
+        load_rows<T>(rows_view(a.Y, r0, left, 4 * D), l, raw.y);
+        if constexpr (GATED) {
+            if (full) load_rows<T>(rows_view(a.G, r0, left, 4 * D), l, raw.g);
+            else fill<T>(raw.g, __builtin_amdgcn_raw_buffer_load_b32(rows_view(a.G, r0, left, 4), l.row * 4, 0, 0));
+        }
+    };
+    load((int64_t)blockIdx.x * T::R);
+    for (int64_t r0 = (int64_t)blockIdx.x * T::R; r0 < end; r0 += step) {
+        const int left = left_of(r0);
+        const bool on = l.row < left;
+        float x[T::E], y[T::E], g[T::E], m, r;
+#pragma unroll
+        for (int i = 0; i < T::E; ++i) {
+            x[i] = of_bits(raw.x[i]);
+            y[i] = of_bits(raw.y[i]);
+            if constexpr (GATED) g[i] = of_bits(raw.g[i]);
+        }
+        load(r0 + step);
         if (a.Y) {
-            float y[T::E], m, r;
-            row_load<T>(a.Y + at, t, D, on, y);
-            row_stats<T>(y, t, D, layer, a.b.eps, m, r);
-            if (a.saved.y.q) row_pack<T>(a.saved.y.q, a.saved.y.scale, row, a.n, t, D, groups, on, y);
-            if (on && t == 0 && a.saved.stats_after) put_stats(a.saved.stats_after, row, layer, m, r);
-            float g[T::E];
-            if (a.b.gate_cols == 0) {
+            row_stats<T>(y, l, sums, D, layer, inv, eps, m, r);
+            store_stats(stats_view(a.saved.stats_after, r0, left, layer), l.row, l.t == 0, layer, m, r);
+            if constexpr (CKPT) {
+                if (a.saved.y.q) store_codes<T>(rows_view(a.saved.y.q, r0, left, D), scales_view(a.saved.y.scale, r0, a.n, groups), l, on, y);
+                if constexpr (GATED)
+                    if (a.saved.g.q) store_codes<T>(rows_view(a.saved.g.q, r0, left, D), scales_view(a.saved.g.scale, r0, a.n, groups), l, on, g);
+            }
+            if constexpr (GATED) {
+                if (full) {
 #pragma unroll
-                for (int i = 0; i < T::E; ++i) g[i] = 1.f;
-            } else if (a.b.gate_cols == D) {
-                row_load<T>(a.G + at, t, D, on, g);
-                if (a.saved.g.q) row_pack<T>(a.saved.g.q, a.saved.g.scale, row, a.n, t, D, groups, on, g);
+                    for (int i = 0; i < T::E; ++i) g[i] = sigmoid(g[i]);
+                } else {
+                    const float one = sigmoid(g[0]);
 #pragma unroll
-                for (int i = 0; i < T::E; ++i) g[i] = sigmoid(g[i]);
-            } else {
-                const float one = on ? sigmoid(a.G[row]) : 0.f;
-#pragma unroll
-                for (int i = 0; i < T::E; ++i) g[i] = one;
+                    for (int i = 0; i < T::E; ++i) g[i] = one;
+                }
             }
 #pragma unroll
-            for (int i = 0; i < T::E; ++i) x[i] = fmaf(sc[i] * g[i], fmaf((y[i] - m) * r, wa[i], ba[i]), x[i]);
-            row_store<T>(a.X_out + at, t, D, on, x);
+            for (int i = 0; i < T::E; ++i) x[i] = fmaf(GATED ? sc[i] * g[i] : sc[i], fmaf((y[i] - m) * r, wa[i], ba[i]), x[i]);
+            store_rows<T>(rows_view(a.X_out, r0, left, 4 * D), l, x);
         }
-        if (a.saved.x.q) row_pack<T>(a.saved.x.q, a.saved.x.scale, row, a.n, t, D, groups, on, x);
+        if constexpr (CKPT)
+            if (a.saved.x.q) store_codes<T>(rows_view(a.saved.x.q, r0, left, D), scales_view(a.saved.x.scale, r0, a.n, groups), l, on, x);
         if (a.N) {
-            float m, r;
-            row_stats<T>(x, t, D, layer, a.b.eps, m, r);
-            if (on && t == 0 && a.saved.stats_before) put_stats(a.saved.stats_before, row, layer, m, r);
+            row_stats<T>(x, l, sums, D, layer, inv, eps, m, r);
+            store_stats(stats_view(a.saved.stats_before, r0, left, layer), l.row, l.t == 0, layer, m, r);
 #pragma unroll
             for (int i = 0; i < T::E; ++i) x[i] = fmaf((x[i] - m) * r, wb[i], bb[i]);
-            row_store<T>(a.N + at, t, D, on, x);
+            store_rows<T>(rows_view(a.N, r0, left, 4 * D), l, x);
         }
     }
 }
 
 // gradient of a norm's input from that of its result: r * (g - [layer] mean(g) - xh * mean(g * xh)), in place of g
-template <typename T> __device__ __forceinline__ void norm_back(float (&g)[T::E], const float (&xh)[T::E], float r, bool layer, float inv) {
+template <typename T>
+__device__ __forceinline__ void norm_back(float (&g)[T::E], const float (&xh)[T::E], RowSums& sums, float r, bool layer, float inv) {
     float s = 0.f, sx = 0.f;
 #pragma unroll
-    for (int i = 0; i < T::E; ++i) {
-        s += g[i];
-        sx = fmaf(g[i], xh[i], sx);
-    }
-    sx = lane_sum<T::LPR>(sx) * inv;
-    s = layer ? lane_sum<T::LPR>(s) * inv : 0.f;
+    for (int i = 0; i < T::E; ++i) sx = fmaf(g[i], xh[i], sx);
+    if (layer) {
 #pragma unroll
-    for (int i = 0; i < T::E; ++i) g[i] = r * (g[i] - s - xh[i] * sx);
+        for (int i = 0; i < T::E; ++i) s += g[i];
+        sums.sum<T>(s, sx);
+        s *= inv;
+    } else {
+        sx = sums.sum<T>(sx);
+    }
+    sx *= inv;
+#pragma unroll
+    for (int i = 0; i < T::E; ++i) g[i] = r * fmaf(-xh[i], sx, g[i] - s);
 }
 
-template <typename T> __global__ __launch_bounds__(kBlockThreads) void block_bwd_kernel(BlockBwd a) {
-    constexpr int R = kBlockThreads / T::LPR;
-    __shared__ float sh[R][T::LPR * T::E];
-    const int t = threadIdx.x % T::LPR, D = a.D, groups = act_groups(D);
-    const bool layer = a.b.norm == DR_ROWNORM_LAYER, after = a.Y || a.saved.y.q;
+// Columns past the width hold whatever the arithmetic makes of zeros: parameters are zeros there, so they add nothing to a row's sums, and
+// they are neither stored nor part of the sums over rows.  Rows past the end are zeros throughout, their statistics among them.
+template <typename T, bool GATED> struct BwdRow {
+    uint32_t d[T::E], n[T::E], x[T::E], y[T::E], g[GATED ? T::E : 1], sx[T::V], sy[T::V], sg[T::V];
+    float m1, r1, m2, r2;
+};
+template <typename T, bool GATED> __global__ __launch_bounds__(kRowThreads) void block_bwd_kernel(BlockBwd a) {
+    __shared__ float sh[2][kRowThreads / kWave][2];
+    __shared__ float all[T::R][T::LPR * T::E];
+    RowSums sums{sh, 0};
+    const int D = a.D, groups = act_groups(D);
+    const RowLane<T> l(D);
+    const bool layer = a.b.norm == DR_ROWNORM_LAYER, full = a.b.gate_cols == D, after = a.Y || a.saved.y.q;
+    const bool x8 = a.saved.x.q != nullptr, y8 = a.saved.y.q != nullptr, g8 = a.saved.g.q != nullptr;
     const float inv = 1.0f / (float)D;
     float wa[T::E], ba[T::E], sc[T::E], wb[T::E];
-    vec_load<T>(a.b.w_after, t, D, 1.f, wa);
-    vec_load<T>(a.b.b_after, t, D, 0.f, ba);
-    vec_load<T>(a.b.scale, t, D, 1.f, sc);
-    vec_load<T>(a.b.w_before, t, D, 1.f, wb);
+    vec_load<T>(a.b.w_after, l, D, 1.f, wa);
+    vec_load<T>(a.b.b_after, l, D, 0.f, ba);
+    vec_load<T>(a.b.scale, l, D, 1.f, sc);
+    vec_load<T>(a.b.w_before, l, D, 1.f, wb);
     float sum[kSums][T::E];
 #pragma unroll
     for (int p = 0; p < kSums; ++p)
 #pragma unroll
         for (int i = 0; i < T::E; ++i) sum[p][i] = 0.f;
-    for (int64_t r0 = (int64_t)blockIdx.x * R; r0 < a.n; r0 += (int64_t)gridDim.x * R) {
-        const int64_t row = r0 + threadIdx.x / T::LPR;
-        const bool on = row < a.n;
-        const size_t at = (size_t)row * D;
-        float d[T::E];
-        if (a.dX_out) {
-            row_load<T>(a.dX_out + at, t, D, on, d);
+    const int64_t step = (int64_t)gridDim.x * T::R;
+    const auto left_of = [&](int64_t r0) { return (int)(a.n - r0 < T::R ? (a.n > r0 ? a.n - r0 : 0) : T::R); };
+    BwdRow<T, GATED> raw;
+    // the same number of loads either way: the compiler counts how many may be outstanding
+    const auto load_either = [&](bool eight, const float* f, const dr_act8& c, int64_t r0, int left, uint32_t (&x)[T::E], uint32_t (&s)[T::V]) {
+        if (eight) {
+            load_codes<T>(rows_view(c.q, r0, left, D), scales_view(c.scale, r0, a.n, groups), l, x, s);
         } else {
+            load_rows<T>(rows_view(f, r0, left, 4 * D), l, x);
 #pragma unroll
-            for (int i = 0; i < T::E; ++i) d[i] = 0.f;
+            for (int v = 0; v < T::V; ++v) s[v] = __builtin_amdgcn_raw_buffer_load_b8(buf_view(nullptr, 0), 0, 0, 0);
         }
-        if (a.dN) {
-            float g[T::E], x[T::E], m = 0.f, r = 0.f;
-            row_load<T>(a.dN + at, t, D, on, g);
-            if (a.X_out) row_load<T>(a.X_out + at, t, D, on, x);
-            else row_unpack<T>(a.saved.x.q, a.saved.x.scale, row, t, D, groups, on, x);
-            if (on) get_stats(a.saved.stats_before, row, layer, m, r);
+    };
+    const auto load = [&](int64_t r0) {
+        const int left = left_of(r0);
+        load_rows<T>(rows_view(a.dX_out, r0, left, 4 * D), l, raw.d);
+        load_rows<T>(rows_view(a.dN, r0, left, 4 * D), l, raw.n);
+        load_either(x8, a.X_out, a.saved.x, r0, left, raw.x, raw.sx);
+        load_either(y8, a.Y, a.saved.y, r0, left, raw.y, raw.sy);
+        load_stats(stats_view(a.saved.stats_before, r0, left, layer), l.row, layer, raw.m1, raw.r1);
+        load_stats(stats_view(a.saved.stats_after, r0, left, layer), l.row, layer, raw.m2, raw.r2);
+        if constexpr (GATED) {
+            if (full) load_either(g8, a.G, a.saved.g, r0, left, raw.g, raw.sg);
+            else fill<T>(raw.g, __builtin_amdgcn_raw_buffer_load_b32(rows_view(a.G, r0, left, 4), l.row * 4, 0, 0));
+        }
+    };
+    load((int64_t)blockIdx.x * T::R);
+    for (int64_t r0 = (int64_t)blockIdx.x * T::R; r0 < a.n; r0 += step) {
+        const int left = left_of(r0);
+        const bool on = l.row < left;
+        float d[T::E], n[T::E], x[T::E], y[T::E], g[T::E];
+        const auto values = [&](bool eight, const uint32_t (&from)[T::E], const uint32_t (&s)[T::V], float (&to)[T::E]) {
+            if (eight) {
+                decode<T>(from, s, on, to);
+            } else {
 #pragma unroll
-            for (int i = 0; i < T::E; ++i) {
-                x[i] = tile_col<T>(t, i / T::W) < D ? (x[i] - m) * r : 0.f;
-                sum[3][i] = fmaf(g[i], x[i], sum[3][i]);
-                sum[4][i] += g[i];
-                g[i] *= wb[i];
+                for (int i = 0; i < T::E; ++i) to[i] = of_bits(from[i]);
             }
-            norm_back<T>(g, x, r, layer, inv);
-#pragma unroll
-            for (int i = 0; i < T::E; ++i) d[i] += g[i];
-        }
-        if (!after) {
-            if (a.grads.dX) row_store<T>(a.grads.dX + at, t, D, on, d);
-            continue;
-        }
-        float y[T::E], g[T::E], m = 0.f, r = 0.f;
-        if (a.Y) row_load<T>(a.Y + at, t, D, on, y);
-        else row_unpack<T>(a.saved.y.q, a.saved.y.scale, row, t, D, groups, on, y);
-        if (on) get_stats(a.saved.stats_after, row, layer, m, r);
-        if (a.b.gate_cols == 0) {
-#pragma unroll
-            for (int i = 0; i < T::E; ++i) g[i] = 1.f;
-        } else if (a.b.gate_cols == D) {
-            if (a.G) row_load<T>(a.G + at, t, D, on, g);
-            else row_unpack<T>(a.saved.g.q, a.saved.g.scale, row, t, D, groups, on, g);
-#pragma unroll
-            for (int i = 0; i < T::E; ++i) g[i] = sigmoid(g[i]);
-        } else {
-            const float one = on ? sigmoid(a.G[row]) : 0.f;
-#pragma unroll
-            for (int i = 0; i < T::E; ++i) g[i] = one;
-        }
-        float dg[T::E], du[T::E], all = 0.f;
+        };
 #pragma unroll
         for (int i = 0; i < T::E; ++i) {
-            const bool in = on && tile_col<T>(t, i / T::W) < D;
-            y[i] = in ? (y[i] - m) * r : 0.f;
-            const float u = fmaf(y[i], wa[i], ba[i]), tt = d[i] * sc[i];
-            du[i] = in ? tt * g[i] : 0.f;
-            dg[i] = in ? tt * u * g[i] * (1.0f - g[i]) : 0.f;
-            all += dg[i];
-            sum[0][i] = fmaf(du[i], y[i], sum[0][i]);
-            sum[1][i] += du[i];
-            sum[2][i] += in ? d[i] * g[i] * u : 0.f;
-            du[i] *= wa[i];
+            d[i] = of_bits(raw.d[i]);
+            n[i] = of_bits(raw.n[i]);
         }
-        if (a.grads.dG) {
-            if (a.b.gate_cols == D) {
-                row_store<T>(a.grads.dG + at, t, D, on, dg);
+        values(x8, raw.x, raw.sx, x);
+        values(y8, raw.y, raw.sy, y);
+        if constexpr (GATED) {
+            if (full) {
+                values(g8, raw.g, raw.sg, g);
+#pragma unroll
+                for (int i = 0; i < T::E; ++i) g[i] = sigmoid(g[i]);
             } else {
-                all = lane_sum<T::LPR>(all);
-                if (on && t == 0) a.grads.dG[row] = all;
+                const float one = sigmoid(of_bits(raw.g[0]));
+#pragma unroll
+                for (int i = 0; i < T::E; ++i) g[i] = one;
             }
         }
-        norm_back<T>(du, y, r, layer, inv);
-        if (a.grads.dX) row_store<T>(a.grads.dX + at, t, D, on, d);       // (the rows that were read may be those that are written)
-        if (a.grads.dY) row_store<T>(a.grads.dY + at, t, D, on, du);
+        const float m1 = raw.m1, r1 = raw.r1, m2 = raw.m2, r2 = raw.r2;
+        load(r0 + step);
+        if (a.dN) {
+#pragma unroll
+            for (int i = 0; i < T::E; ++i) {
+                x[i] = (x[i] - m1) * r1;
+                sum[3][i] = fmaf(n[i], x[i], sum[3][i]);
+                sum[4][i] += n[i];
+                n[i] *= wb[i];
+            }
+            norm_back<T>(n, x, sums, r1, layer, inv);
+#pragma unroll
+            for (int i = 0; i < T::E; ++i) d[i] += n[i];
+        }
+        store_rows<T>(rows_view(a.grads.dX, r0, left, 4 * D), l, d);
+        if (!after) continue;
+        float dg[T::E], du[T::E], row = 0.f;
+#pragma unroll
+        for (int i = 0; i < T::E; ++i) {
+            y[i] = (y[i] - m2) * r2;
+            const float u = fmaf(y[i], wa[i], ba[i]), t = d[i] * sc[i];
+            if constexpr (GATED) {
+                const float dgate = d[i] * g[i];
+                du[i] = t * g[i];
+                dg[i] = du[i] * u * (1.0f - g[i]);
+                sum[2][i] = fmaf(dgate, u, sum[2][i]);
+            } else {
+                du[i] = t;
+                sum[2][i] = fmaf(d[i], u, sum[2][i]);
+            }
+            sum[0][i] = fmaf(du[i], y[i], sum[0][i]);
+            sum[1][i] += du[i];
+            du[i] *= wa[i];
+        }
+        if constexpr (GATED) {
+            if (full) {
+                store_rows<T>(rows_view(a.grads.dG, r0, left, 4 * D), l, dg);
+            } else {
+#pragma unroll
+                for (int i = 0; i < T::E; ++i) row += dg[i];
+                row = sums.sum<T>(row);
+                __builtin_amdgcn_raw_buffer_store_b32(bits(row), rows_view(a.grads.dG, r0, left, 4), l.t == 0 ? l.row * 4 : kOutside, 0, 0);
+            }
+        }
+        norm_back<T>(du, y, sums, r2, layer, inv);
+        store_rows<T>(rows_view(a.grads.dY, r0, left, 4 * D), l, du);
     }
+    float* const part = a.part + (size_t)blockIdx.x * kSums * D;
     for (int p = 0; p < kSums; ++p) {
         __syncthreads();
 #pragma unroll
         for (int v = 0; v < T::V; ++v)
 #pragma unroll
-            for (int j = 0; j < T::W; ++j) sh[threadIdx.x / T::LPR][tile_col<T>(t, v) + j] = sum[p][T::W * v + j];
+            for (int j = 0; j < T::W; ++j) all[l.row][l.col(v) + j] = sum[p][T::W * v + j];
         __syncthreads();
-        for (int c = threadIdx.x; c < D; c += kBlockThreads) {
+        for (int c = threadIdx.x; c < D; c += kRowThreads) {
             float s = 0.f;
 #pragma unroll
-            for (int k = 0; k < R; ++k) s += sh[k][c];
-            a.part[((size_t)blockIdx.x * kSums + p) * D + c] = s;
+            for (int k = 0; k < T::R; ++k) s += all[k][c];
+            part[(size_t)p * D + c] = s;
         }
     }
 }
 
-// the five sums over the workgroups' partials, in 64 bits and a fixed order
-__global__ __launch_bounds__(256) void block_sums_kernel(const float* __restrict__ part, int parts, int D, dr_block_grads g) {
-    const int i = blockIdx.x * 256 + threadIdx.x;
-    if (i >= kSums * D) return;
+// The five sums over the workgroups' partials, in 64 bits and a fixed order: a wavefront sums every sixteenth partial of 64 columns, the
+// sixteen sums are added in order.
+constexpr int kSumWaves = 16, kSumAhead = 8;
+__global__ __launch_bounds__(kWave* kSumWaves) void block_sums_kernel(const float* part, int parts, int D, dr_block_grads g) {
+    __shared__ double sh[kSumWaves][kWave];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, count = kSums * D, i = blockIdx.x * kWave + lane;
+    const float* const src = part + min(i, count - 1);
+    double s = 0.0;
+    int p = wave;
+    for (; p + (kSumAhead - 1) * kSumWaves < parts; p += kSumAhead * kSumWaves) {
+        float v[kSumAhead];
+#pragma unroll
+        for (int u = 0; u < kSumAhead; ++u) v[u] = src[(size_t)(p + u * kSumWaves) * count];
+#pragma unroll
+        for (int u = 0; u < kSumAhead; ++u) s += (double)v[u];
+    }
+    for (; p < parts; p += kSumWaves) s += (double)src[(size_t)p * count];
+    sh[wave][lane] = s;
+    __syncthreads();
+    if (wave != 0 || i >= count) return;
     float* const to[kSums] = {g.dw_after, g.db_after, g.dscale, g.dw_before, g.db_before};
     float* const o = to[i / D];
     if (!o) return;
-    double s = 0.0;
-    for (int p = 0; p < parts; ++p) s += (double)part[(size_t)p * kSums * D + i];
+    s = sh[0][lane];
+#pragma unroll
+    for (int w = 1; w < kSumWaves; ++w) s += sh[w][lane];
     o[i % D] = (float)s;
 }
 
-constexpr int kBwdWgs = 1024;
+constexpr int kFwdWgs = 2048, kBwdWgs = 1024;
 static bool vector_rows(int D, std::initializer_list<const void*> f32, std::initializer_list<const void*> q) {
     bool v = D % 4 == 0;
     for (const void* p : f32) v = v && aligned(p, 16);
@@ -251,11 +352,19 @@ static bool vector_rows(int D, std::initializer_list<const void*> f32, std::init
 
 int launch_block_fwd(const BlockFwd& a, hipStream_t s) {
     const bool vector = vector_rows(a.D, {a.X, a.Y, a.b.gate_cols == a.D ? a.G : nullptr, a.X_out, a.N}, {a.saved.x.q, a.saved.y.q, a.saved.g.q});
+    const bool ckpt = a.saved.x.q || a.saved.y.q || a.saved.g.q;
     return with_row_tile(a.D, vector, [&](auto tile) -> int {
         using T = decltype(tile);
-        constexpr int R = kBlockThreads / T::LPR;
-        const int64_t blocks = (a.n + R - 1) / R;
-        hipLaunchKernelGGL((block_fwd_kernel<T>), dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(kBlockThreads), 0, s, a);
+        const int64_t rows = ckpt ? (a.n + 7) / 8 * 8 : a.n, blocks = (rows + T::R - 1) / T::R;
+        const dim3 grid((unsigned)(blocks < kFwdWgs ? blocks : kFwdWgs));
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kRowThreads), 0, s, a); };
+        if (a.G) {
+            if (ckpt) go(block_fwd_kernel<T, true, true>);
+            else go(block_fwd_kernel<T, true, false>);
+        } else {
+            if (ckpt) go(block_fwd_kernel<T, false, true>);
+            else go(block_fwd_kernel<T, false, false>);
+        }
         DRC_HIP(hipGetLastError());
         return DR_OK;
     });
@@ -275,16 +384,17 @@ int launch_block_bwd(BlockBwd a, void* ws, hipStream_t s) {
     if (a.n > 0)
         DRC_TRY(with_row_tile(a.D, vector, [&](auto tile) -> int {
             using T = decltype(tile);
-            constexpr int R = kBlockThreads / T::LPR;
-            const int64_t blocks = (a.n + R - 1) / R;
+            const int64_t blocks = (a.n + T::R - 1) / T::R;
             a.parts = (int)(blocks < kBwdWgs ? blocks : kBwdWgs);
-            hipLaunchKernelGGL((block_bwd_kernel<T>), dim3((unsigned)a.parts), dim3(kBlockThreads), 0, s, a);
+            auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)a.parts), dim3(kRowThreads), 0, s, a); };
+            if (a.b.gate_cols) go(block_bwd_kernel<T, true>);
+            else go(block_bwd_kernel<T, false>);
             DRC_HIP(hipGetLastError());
             return DR_OK;
         }));
     const dr_block_grads& g = a.grads;
     if (g.dw_after || g.db_after || g.dscale || g.dw_before || g.db_before) {
-        hipLaunchKernelGGL(block_sums_kernel, dim3((unsigned)((kSums * a.D + 255) / 256)), dim3(256), 0, s, a.part, a.parts, a.D, g);
+        hipLaunchKernelGGL(block_sums_kernel, dim3((unsigned)((kSums * a.D + kWave - 1) / kWave)), dim3(kWave * kSumWaves), 0, s, a.part, a.parts, a.D, g);
         DRC_HIP(hipGetLastError());
     }
     return DR_OK;
