@@ -277,8 +277,8 @@ def _act8(ckpt) -> dr_act8:
 
 
 def _stream_of(stream) -> int:
-    if stream is None:
-        stream = torch.cuda.current_stream()
+    if stream is None:        # the current stream's handle, without a torch.cuda.Stream around it (2.7 us of a call)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 

@@ -136,13 +136,23 @@ template <typename T> __device__ __forceinline__ void load_rows(Buf b, const Row
         }
     }
 }
-template <typename T> __device__ __forceinline__ void store_rows(Buf b, const RowLane<T>& l, const float (&x)[T::E]) {
+// Elements in registers of their own: the loads of the next rows can then go where these came from.  (Left to itself the compiler loads the
+// next rows elsewhere and copies them, which waits for the loads that have just been issued.)
+template <int N> __device__ __forceinline__ void take(const uint32_t (&from)[N], float (&to)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        to[i] = of_bits(from[i]);
+        asm volatile("" : "+v"(to[i]));
+    }
+}
+constexpr int kStreamed = 2;      // cache policy of stores that nothing is to be read from soon
+template <typename T, int POLICY = 0> __device__ __forceinline__ void store_rows(Buf b, const RowLane<T>& l, const float (&x)[T::E]) {
 #pragma unroll
     for (int v = 0; v < T::V; ++v) {
         if constexpr (T::W == 4)
-            __builtin_amdgcn_raw_buffer_store_b128(u32x4{bits(x[4 * v]), bits(x[4 * v + 1]), bits(x[4 * v + 2]), bits(x[4 * v + 3])}, b, l.at[v], 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b128(u32x4{bits(x[4 * v]), bits(x[4 * v + 1]), bits(x[4 * v + 2]), bits(x[4 * v + 3])}, b, l.at[v], 0, POLICY);
         else
-            __builtin_amdgcn_raw_buffer_store_b32(bits(x[v]), b, l.at[v], 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b32(bits(x[v]), b, l.at[v], 0, POLICY);
     }
 }
 

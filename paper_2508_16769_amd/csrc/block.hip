@@ -11,6 +11,7 @@
 #include "act8.h"
 
 #include <initializer_list>
+#include <type_traits>
 
 namespace drc {
 
@@ -51,100 +52,83 @@ __device__ __forceinline__ void row_stats(const float (&x)[T::E], const RowLane<
 }
 __device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.0f + expf(-g)); }
 
-// Statistics are [n] or [n,2]: one load or store either way.
+// Statistics are [n] (r) or [n,2] (m, r).  A mean that is not there is read from outside, as zero.
+struct StatsLane {
+    int m, r;
+    __device__ __forceinline__ StatsLane(int row, bool layer, bool on) : m(on && layer ? row * 8 : kOutside), r(on ? (layer ? row * 8 + 4 : row * 4) : kOutside) {}
+};
 __device__ __forceinline__ Buf stats_view(const float* p, int64_t r0, int left, bool layer) { return rows_view(p, r0, left, layer ? 8 : 4); }
-__device__ __forceinline__ void load_stats(Buf b, int row, bool layer, float& m, float& r) {
-    if (layer) {
-        const u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(b, row * 8, 0, 0));
-        m = of_bits(v[0]);
-        r = of_bits(v[1]);
-    } else {
-        m = 0.f;
-        r = of_bits(__builtin_amdgcn_raw_buffer_load_b32(b, row * 4, 0, 0));
-    }
-}
-__device__ __forceinline__ void store_stats(Buf b, int row, bool first, bool layer, float m, float r) {
-    if (layer) __builtin_amdgcn_raw_buffer_store_b64(u32x2{bits(m), bits(r)}, b, first ? row * 8 : kOutside, 0, 0);
-    else __builtin_amdgcn_raw_buffer_store_b32(bits(r), b, first ? row * 4 : kOutside, 0, 0);
-}
 
-template <typename T> __device__ __forceinline__ void fill(uint32_t (&x)[T::E], uint32_t v) {
-#pragma unroll
-    for (int i = 0; i < T::E; ++i) x[i] = v;
-}
-
-// What a row brings, as it comes from memory: loaded a block of rows ahead.
-template <typename T, bool GATED> struct FwdRow { uint32_t x[T::E], y[T::E], g[GATED ? T::E : 1]; };
+// The loops below have no memory access under a condition: what is absent has an empty view.  The compiler then knows how many loads and stores
+// are outstanding wherever it has to wait for some of them; with branches around loads and stores every row waited for the loads of
+// the next one (1.2 M x 128 backward from checkpoints, two workgroups per compute unit: 627 us, now 496).
+// A row's loads do wait for the stores of the row before, and that is left as it is: with as many empty stores in front of the loop as it ends with
+// the compiler lets them pass, and workgroups then spread over more of memory's pages (forward 443 / 456, backward 496 / 540 us).
+enum Gate { kNoGate, kRowGate, kFullGate };
+__device__ __forceinline__ int rows_left(int64_t n, int64_t r0, int rows) { return (int)(n - r0 < rows ? (n > r0 ? n - r0 : 0) : rows); }
 
 // CKPT: checkpoints are kept (of any of the three tensors).
-template <typename T, bool GATED, bool CKPT> __global__ __launch_bounds__(kRowThreads) void block_fwd_kernel(BlockFwd a) {
+template <typename T, int GATE, bool CKPT> __global__ __launch_bounds__(kRowThreads) void block_fwd_kernel(BlockFwd a) {
     __shared__ float sh[2][kRowThreads / kWave][2];
     RowSums sums{sh, 0};
     const int D = a.D, groups = act_groups(D);
     const RowLane<T> l(D);
-    const bool layer = a.b.norm == DR_ROWNORM_LAYER, full = a.b.gate_cols == D;
+    const bool layer = a.b.norm == DR_ROWNORM_LAYER;
+    const StatsLane st(l.row, layer, l.t == 0);
     const float inv = 1.0f / (float)D, eps = a.b.eps;
     float wa[T::E], ba[T::E], sc[T::E], wb[T::E], bb[T::E];
-    vec_load<T>(a.b.w_after, l, D, 1.f, wa);
-    vec_load<T>(a.b.b_after, l, D, 0.f, ba);
-    vec_load<T>(a.b.scale, l, D, 1.f, sc);
+    vec_load<T>(a.Y ? a.b.w_after : nullptr, l, D, a.Y ? 1.f : 0.f, wa);     // without Y, X_out is X
+    vec_load<T>(a.Y ? a.b.b_after : nullptr, l, D, 0.f, ba);
+    vec_load<T>(a.Y ? a.b.scale : nullptr, l, D, a.Y ? 1.f : 0.f, sc);
     vec_load<T>(a.b.w_before, l, D, 1.f, wb);
     vec_load<T>(a.b.b_before, l, D, 0.f, bb);
     const int64_t end = CKPT ? (a.n + 7) & ~int64_t(7) : a.n, step = (int64_t)gridDim.x * T::R;
-    const auto left_of = [&](int64_t r0) { return (int)(a.n - r0 < T::R ? (a.n > r0 ? a.n - r0 : 0) : T::R); };
-    FwdRow<T, GATED> raw;
+    uint32_t rx[T::E], ry[T::E], rg[T::E], r1;                  // what the next rows bring
     const auto load = [&](int64_t r0) {
-        const int left = left_of(r0);
-        load_rows<T>(rows_view(a.X, r0, left, 4 * D), l, raw.x);
-        load_rows<T>(rows_view(a.Y, r0, left, 4 * D), l, raw.y);
-        if constexpr (GATED) {
-            if (full) load_rows<T>(rows_view(a.G, r0, left, 4 * D), l, raw.g);
-            else fill<T>(raw.g, __builtin_amdgcn_raw_buffer_load_b32(rows_view(a.G, r0, left, 4), l.row * 4, 0, 0));
-        }
+        const int left = rows_left(a.n, r0, T::R);
+        load_rows<T>(rows_view(a.X, r0, left, 4 * D), l, rx);
+        load_rows<T>(rows_view(a.Y, r0, left, 4 * D), l, ry);
+        if constexpr (GATE == kFullGate) load_rows<T>(rows_view(a.G, r0, left, 4 * D), l, rg);
+        if constexpr (GATE == kRowGate) r1 = __builtin_amdgcn_raw_buffer_load_b32(rows_view(a.G, r0, left, 4), l.row * 4, 0, 0);
     };
     load((int64_t)blockIdx.x * T::R);
     for (int64_t r0 = (int64_t)blockIdx.x * T::R; r0 < end; r0 += step) {
-        const int left = left_of(r0);
+        const int left = rows_left(a.n, r0, T::R);
         const bool on = l.row < left;
         float x[T::E], y[T::E], g[T::E], m, r;
+        take(rx, x);
+        take(ry, y);
+        if constexpr (GATE == kFullGate) take(rg, g);
+        if constexpr (GATE == kRowGate) {
+            const float one = sigmoid(of_bits(r1));
 #pragma unroll
-        for (int i = 0; i < T::E; ++i) {
-            x[i] = of_bits(raw.x[i]);
-            y[i] = of_bits(raw.y[i]);
-            if constexpr (GATED) g[i] = of_bits(raw.g[i]);
+            for (int i = 0; i < T::E; ++i) g[i] = one;
         }
         load(r0 + step);
-        if (a.Y) {
-            row_stats<T>(y, l, sums, D, layer, inv, eps, m, r);
-            store_stats(stats_view(a.saved.stats_after, r0, left, layer), l.row, l.t == 0, layer, m, r);
-            if constexpr (CKPT) {
-                if (a.saved.y.q) store_codes<T>(rows_view(a.saved.y.q, r0, left, D), scales_view(a.saved.y.scale, r0, a.n, groups), l, on, y);
-                if constexpr (GATED)
-                    if (a.saved.g.q) store_codes<T>(rows_view(a.saved.g.q, r0, left, D), scales_view(a.saved.g.scale, r0, a.n, groups), l, on, g);
-            }
-            if constexpr (GATED) {
-                if (full) {
-#pragma unroll
-                    for (int i = 0; i < T::E; ++i) g[i] = sigmoid(g[i]);
-                } else {
-                    const float one = sigmoid(g[0]);
-#pragma unroll
-                    for (int i = 0; i < T::E; ++i) g[i] = one;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < T::E; ++i) x[i] = fmaf(GATED ? sc[i] * g[i] : sc[i], fmaf((y[i] - m) * r, wa[i], ba[i]), x[i]);
-            store_rows<T>(rows_view(a.X_out, r0, left, 4 * D), l, x);
+        row_stats<T>(y, l, sums, D, layer, inv, eps, m, r);
+        const Buf sa = stats_view(a.saved.stats_after, r0, left, layer);
+        __builtin_amdgcn_raw_buffer_store_b32(bits(m), sa, st.m, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b32(bits(r), sa, st.r, 0, 0);
+        if constexpr (CKPT) {
+            store_codes<T>(rows_view(a.saved.y.q, r0, left, D), scales_view(a.saved.y.scale, r0, a.n, groups), l, on, y);
+            if constexpr (GATE == kFullGate)
+                store_codes<T>(rows_view(a.saved.g.q, r0, left, D), scales_view(a.saved.g.scale, r0, a.n, groups), l, on, g);
         }
-        if constexpr (CKPT)
-            if (a.saved.x.q) store_codes<T>(rows_view(a.saved.x.q, r0, left, D), scales_view(a.saved.x.scale, r0, a.n, groups), l, on, x);
-        if (a.N) {
-            row_stats<T>(x, l, sums, D, layer, inv, eps, m, r);
-            store_stats(stats_view(a.saved.stats_before, r0, left, layer), l.row, l.t == 0, layer, m, r);
+        if constexpr (GATE == kFullGate) {
 #pragma unroll
-            for (int i = 0; i < T::E; ++i) x[i] = fmaf((x[i] - m) * r, wb[i], bb[i]);
-            store_rows<T>(rows_view(a.N, r0, left, 4 * D), l, x);
+            for (int i = 0; i < T::E; ++i) g[i] = sigmoid(g[i]);
         }
+#pragma unroll
+        for (int i = 0; i < T::E; ++i) x[i] = fmaf(GATE != kNoGate ? sc[i] * g[i] : sc[i], fmaf((y[i] - m) * r, wa[i], ba[i]), x[i]);
+        store_rows<T>(rows_view(a.X_out, r0, left, 4 * D), l, x);
+        if constexpr (CKPT) store_codes<T>(rows_view(a.saved.x.q, r0, left, D), scales_view(a.saved.x.scale, r0, a.n, groups), l, on, x);
+        row_stats<T>(x, l, sums, D, layer, inv, eps, m, r);
+        const Buf sb = stats_view(a.saved.stats_before, r0, left, layer);
+        __builtin_amdgcn_raw_buffer_store_b32(bits(m), sb, st.m, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b32(bits(r), sb, st.r, 0, 0);
+#pragma unroll
+        for (int i = 0; i < T::E; ++i) x[i] = fmaf((x[i] - m) * r, wb[i], bb[i]);
+        store_rows<T>(rows_view(a.N, r0, left, 4 * D), l, x);
     }
 }
 
@@ -167,20 +151,40 @@ __device__ __forceinline__ void norm_back(float (&g)[T::E], const float (&xh)[T:
     for (int i = 0; i < T::E; ++i) g[i] = r * fmaf(-xh[i], sx, g[i] - s);
 }
 
-// Columns past the width hold whatever the arithmetic makes of zeros: parameters are zeros there, so they add nothing to a row's sums, and
-// they are neither stored nor part of the sums over rows.  Rows past the end are zeros throughout, their statistics among them.
-template <typename T, bool GATED> struct BwdRow {
-    uint32_t d[T::E], n[T::E], x[T::E], y[T::E], g[GATED ? T::E : 1], sx[T::V], sy[T::V], sg[T::V];
-    float m1, r1, m2, r2;
+// A tensor's rows of which nothing, fp32 elements or codes are there
+enum From { kFloats, kCodes, kEither };
+template <typename T, int FROM> struct Incoming {
+    uint32_t f[T::E], q[T::E], s[T::V];
+    __device__ __forceinline__ void load(const float* p, const dr_act8& c, const RowLane<T>& l, int64_t r0, int left, int64_t n, int D, int groups) {
+        if constexpr (FROM != kCodes) load_rows<T>(rows_view(p, r0, left, 4 * D), l, f);
+        if constexpr (FROM != kFloats) load_codes<T>(rows_view(c.q, r0, left, D), scales_view(c.scale, r0, n, groups), l, q, s);
+    }
+    __device__ __forceinline__ void get(bool on, float (&x)[T::E]) const {
+        if constexpr (FROM == kFloats) {
+            take(f, x);
+        } else {
+            decode<T>(q, s, on, x);
+            if constexpr (FROM == kEither) {                    // the other one is zeros
+                float y[T::E];
+                take(f, y);
+#pragma unroll
+                for (int i = 0; i < T::E; ++i) x[i] += y[i];
+            }
+        }
+    }
 };
-template <typename T, bool GATED> __global__ __launch_bounds__(kRowThreads) void block_bwd_kernel(BlockBwd a) {
+
+// Columns past the width hold whatever the arithmetic makes of zeros: parameters are zeros there, so they add nothing to a row's sums, and
+// they are neither stored nor part of the sums over rows.  Rows past the end are zeros throughout, their statistics among them; so is all that
+// belongs to a part that is left out.
+template <typename T, int GATE, int FROM> __global__ __launch_bounds__(kRowThreads) void block_bwd_kernel(BlockBwd a) {
     __shared__ float sh[2][kRowThreads / kWave][2];
     __shared__ float all[T::R][T::LPR * T::E];
     RowSums sums{sh, 0};
     const int D = a.D, groups = act_groups(D);
     const RowLane<T> l(D);
-    const bool layer = a.b.norm == DR_ROWNORM_LAYER, full = a.b.gate_cols == D, after = a.Y || a.saved.y.q;
-    const bool x8 = a.saved.x.q != nullptr, y8 = a.saved.y.q != nullptr, g8 = a.saved.g.q != nullptr;
+    const bool layer = a.b.norm == DR_ROWNORM_LAYER;
+    const StatsLane st(l.row, layer, true);
     const float inv = 1.0f / (float)D;
     float wa[T::E], ba[T::E], sc[T::E], wb[T::E];
     vec_load<T>(a.b.w_after, l, D, 1.f, wa);
@@ -193,107 +197,81 @@ template <typename T, bool GATED> __global__ __launch_bounds__(kRowThreads) void
 #pragma unroll
         for (int i = 0; i < T::E; ++i) sum[p][i] = 0.f;
     const int64_t step = (int64_t)gridDim.x * T::R;
-    const auto left_of = [&](int64_t r0) { return (int)(a.n - r0 < T::R ? (a.n > r0 ? a.n - r0 : 0) : T::R); };
-    BwdRow<T, GATED> raw;
-    // the same number of loads either way: the compiler counts how many may be outstanding
-    const auto load_either = [&](bool eight, const float* f, const dr_act8& c, int64_t r0, int left, uint32_t (&x)[T::E], uint32_t (&s)[T::V]) {
-        if (eight) {
-            load_codes<T>(rows_view(c.q, r0, left, D), scales_view(c.scale, r0, a.n, groups), l, x, s);
-        } else {
-            load_rows<T>(rows_view(f, r0, left, 4 * D), l, x);
-#pragma unroll
-            for (int v = 0; v < T::V; ++v) s[v] = __builtin_amdgcn_raw_buffer_load_b8(buf_view(nullptr, 0), 0, 0, 0);
-        }
-    };
+    // what the next rows bring
+    uint32_t rd[T::E], rn[T::E], rs[4], rone;
+    Incoming<T, FROM> ix, iy, ig;
     const auto load = [&](int64_t r0) {
-        const int left = left_of(r0);
-        load_rows<T>(rows_view(a.dX_out, r0, left, 4 * D), l, raw.d);
-        load_rows<T>(rows_view(a.dN, r0, left, 4 * D), l, raw.n);
-        load_either(x8, a.X_out, a.saved.x, r0, left, raw.x, raw.sx);
-        load_either(y8, a.Y, a.saved.y, r0, left, raw.y, raw.sy);
-        load_stats(stats_view(a.saved.stats_before, r0, left, layer), l.row, layer, raw.m1, raw.r1);
-        load_stats(stats_view(a.saved.stats_after, r0, left, layer), l.row, layer, raw.m2, raw.r2);
-        if constexpr (GATED) {
-            if (full) load_either(g8, a.G, a.saved.g, r0, left, raw.g, raw.sg);
-            else fill<T>(raw.g, __builtin_amdgcn_raw_buffer_load_b32(rows_view(a.G, r0, left, 4), l.row * 4, 0, 0));
-        }
+        const int left = rows_left(a.n, r0, T::R);
+        load_rows<T>(rows_view(a.dN, r0, left, 4 * D), l, rn);
+        ix.load(a.X_out, a.saved.x, l, r0, left, a.n, D, groups);
+        const Buf sb = stats_view(a.saved.stats_before, r0, left, layer), sa = stats_view(a.saved.stats_after, r0, left, layer);
+        rs[0] = __builtin_amdgcn_raw_buffer_load_b32(sb, st.m, 0, 0);
+        rs[1] = __builtin_amdgcn_raw_buffer_load_b32(sb, st.r, 0, 0);
+        load_rows<T>(rows_view(a.dX_out, r0, left, 4 * D), l, rd);
+        iy.load(a.Y, a.saved.y, l, r0, left, a.n, D, groups);
+        rs[2] = __builtin_amdgcn_raw_buffer_load_b32(sa, st.m, 0, 0);
+        rs[3] = __builtin_amdgcn_raw_buffer_load_b32(sa, st.r, 0, 0);
+        if constexpr (GATE == kFullGate) ig.load(a.G, a.saved.g, l, r0, left, a.n, D, groups);
+        if constexpr (GATE == kRowGate) rone = __builtin_amdgcn_raw_buffer_load_b32(rows_view(a.G, r0, left, 4), l.row * 4, 0, 0);
     };
     load((int64_t)blockIdx.x * T::R);
     for (int64_t r0 = (int64_t)blockIdx.x * T::R; r0 < a.n; r0 += step) {
-        const int left = left_of(r0);
+        const int left = rows_left(a.n, r0, T::R);
         const bool on = l.row < left;
-        float d[T::E], n[T::E], x[T::E], y[T::E], g[T::E];
-        const auto values = [&](bool eight, const uint32_t (&from)[T::E], const uint32_t (&s)[T::V], float (&to)[T::E]) {
-            if (eight) {
-                decode<T>(from, s, on, to);
-            } else {
+        float d[T::E], n[T::E], x[T::E], y[T::E], g[T::E], s[4];
+        take(rn, n);
+        take(rd, d);
+        take(rs, s);
+        ix.get(on, x);
+        iy.get(on, y);
+        if constexpr (GATE == kFullGate) {
+            ig.get(on, g);
 #pragma unroll
-                for (int i = 0; i < T::E; ++i) to[i] = of_bits(from[i]);
-            }
-        };
-#pragma unroll
-        for (int i = 0; i < T::E; ++i) {
-            d[i] = of_bits(raw.d[i]);
-            n[i] = of_bits(raw.n[i]);
+            for (int i = 0; i < T::E; ++i) g[i] = sigmoid(g[i]);
         }
-        values(x8, raw.x, raw.sx, x);
-        values(y8, raw.y, raw.sy, y);
-        if constexpr (GATED) {
-            if (full) {
-                values(g8, raw.g, raw.sg, g);
+        if constexpr (GATE == kRowGate) {
+            const float one = sigmoid(of_bits(rone));
 #pragma unroll
-                for (int i = 0; i < T::E; ++i) g[i] = sigmoid(g[i]);
-            } else {
-                const float one = sigmoid(of_bits(raw.g[0]));
-#pragma unroll
-                for (int i = 0; i < T::E; ++i) g[i] = one;
-            }
+            for (int i = 0; i < T::E; ++i) g[i] = one;
         }
-        const float m1 = raw.m1, r1 = raw.r1, m2 = raw.m2, r2 = raw.r2;
         load(r0 + step);
-        if (a.dN) {
-#pragma unroll
-            for (int i = 0; i < T::E; ++i) {
-                x[i] = (x[i] - m1) * r1;
-                sum[3][i] = fmaf(n[i], x[i], sum[3][i]);
-                sum[4][i] += n[i];
-                n[i] *= wb[i];
-            }
-            norm_back<T>(n, x, sums, r1, layer, inv);
-#pragma unroll
-            for (int i = 0; i < T::E; ++i) d[i] += n[i];
-        }
-        store_rows<T>(rows_view(a.grads.dX, r0, left, 4 * D), l, d);
-        if (!after) continue;
-        float dg[T::E], du[T::E], row = 0.f;
 #pragma unroll
         for (int i = 0; i < T::E; ++i) {
-            y[i] = (y[i] - m2) * r2;
-            const float u = fmaf(y[i], wa[i], ba[i]), t = d[i] * sc[i];
-            if constexpr (GATED) {
-                const float dgate = d[i] * g[i];
-                du[i] = t * g[i];
+            x[i] = (x[i] - s[0]) * s[1];
+            sum[3][i] = fmaf(n[i], x[i], sum[3][i]);
+            sum[4][i] += n[i];
+            n[i] *= wb[i];
+        }
+        norm_back<T>(n, x, sums, s[1], layer, inv);
+#pragma unroll
+        for (int i = 0; i < T::E; ++i) d[i] += n[i];
+        store_rows<T>(rows_view(a.grads.dX, r0, left, 4 * D), l, d);
+        float dg[T::E], du[T::E];
+#pragma unroll
+        for (int i = 0; i < T::E; ++i) {
+            y[i] = (y[i] - s[2]) * s[3];
+            const float u = fmaf(y[i], wa[i], ba[i]);
+            du[i] = d[i] * sc[i];
+            if constexpr (GATE != kNoGate) {
+                du[i] *= g[i];
                 dg[i] = du[i] * u * (1.0f - g[i]);
-                sum[2][i] = fmaf(dgate, u, sum[2][i]);
+                sum[2][i] = fmaf(d[i] * g[i], u, sum[2][i]);
             } else {
-                du[i] = t;
                 sum[2][i] = fmaf(d[i], u, sum[2][i]);
             }
             sum[0][i] = fmaf(du[i], y[i], sum[0][i]);
             sum[1][i] += du[i];
             du[i] *= wa[i];
         }
-        if constexpr (GATED) {
-            if (full) {
-                store_rows<T>(rows_view(a.grads.dG, r0, left, 4 * D), l, dg);
-            } else {
+        if constexpr (GATE == kFullGate) store_rows<T>(rows_view(a.grads.dG, r0, left, 4 * D), l, dg);
+        if constexpr (GATE == kRowGate) {
+            float row = 0.f;
 #pragma unroll
-                for (int i = 0; i < T::E; ++i) row += dg[i];
-                row = sums.sum<T>(row);
-                __builtin_amdgcn_raw_buffer_store_b32(bits(row), rows_view(a.grads.dG, r0, left, 4), l.t == 0 ? l.row * 4 : kOutside, 0, 0);
-            }
+            for (int i = 0; i < T::E; ++i) row += dg[i];
+            row = sums.sum<T>(row);
+            __builtin_amdgcn_raw_buffer_store_b32(bits(row), rows_view(a.grads.dG, r0, left, 4), l.t == 0 ? l.row * 4 : kOutside, 0, 0);
         }
-        norm_back<T>(du, y, sums, r2, layer, inv);
+        norm_back<T>(du, y, sums, s[3], layer, inv);
         store_rows<T>(rows_view(a.grads.dY, r0, left, 4 * D), l, du);
     }
     float* const part = a.part + (size_t)blockIdx.x * kSums * D;
@@ -342,12 +320,22 @@ __global__ __launch_bounds__(kWave* kSumWaves) void block_sums_kernel(const floa
     o[i % D] = (float)s;
 }
 
-constexpr int kFwdWgs = 2048, kBwdWgs = 1024;
+// Workgroups of a launch: few that walk many rows.  Two per compute unit draw 5.6 TB/s from memory, more of them drift apart and find its
+// pages closed: 1.2 M x 128, 512 / 768 / 1024 / 2048 workgroups, us: forward 443 / 486 / 530 / 580, backward from checkpoints 496 / 552 / 590 /
+// 610; 60 000 x 128 24.4 / 25.4 / 25.7 / 26.0 and 32.8 / 34.5 / 35.5 / 39.4; 256 leave a SIMD one wavefront (528 and 605).  Rows of any width have a
+// quarter as much in flight per lane: 200 000 x 77, 512 / 1024 / 2048: 95 / 61 / 69 and 119 / 91 / 98.
+template <typename T> constexpr int kBlockWgs = T::W == 4 ? 512 : 1024;
 static bool vector_rows(int D, std::initializer_list<const void*> f32, std::initializer_list<const void*> q) {
     bool v = D % 4 == 0;
     for (const void* p : f32) v = v && aligned(p, 16);
     for (const void* p : q) v = v && aligned(p, 4);
     return v;
+}
+
+template <typename F> static void by_gate(int gate_cols, int D, F go) {
+    if (gate_cols == 0) go(std::integral_constant<int, kNoGate>{});
+    else if (gate_cols == D) go(std::integral_constant<int, kFullGate>{});
+    else go(std::integral_constant<int, kRowGate>{});
 }
 
 int launch_block_fwd(const BlockFwd& a, hipStream_t s) {
@@ -356,28 +344,33 @@ int launch_block_fwd(const BlockFwd& a, hipStream_t s) {
     return with_row_tile(a.D, vector, [&](auto tile) -> int {
         using T = decltype(tile);
         const int64_t rows = ckpt ? (a.n + 7) / 8 * 8 : a.n, blocks = (rows + T::R - 1) / T::R;
-        const dim3 grid((unsigned)(blocks < kFwdWgs ? blocks : kFwdWgs));
-        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kRowThreads), 0, s, a); };
-        if (a.G) {
-            if (ckpt) go(block_fwd_kernel<T, true, true>);
-            else go(block_fwd_kernel<T, true, false>);
-        } else {
-            if (ckpt) go(block_fwd_kernel<T, false, true>);
-            else go(block_fwd_kernel<T, false, false>);
-        }
+        const dim3 grid((unsigned)(blocks < kBlockWgs<T> ? blocks : kBlockWgs<T>));
+        auto go = [&](auto gate) {
+            constexpr int GATE = decltype(gate)::value;
+            if (ckpt) hipLaunchKernelGGL((block_fwd_kernel<T, GATE, true>), grid, dim3(kRowThreads), 0, s, a);
+            else hipLaunchKernelGGL((block_fwd_kernel<T, GATE, false>), grid, dim3(kRowThreads), 0, s, a);
+        };
+        by_gate(a.b.gate_cols, a.D, go);
         DRC_HIP(hipGetLastError());
         return DR_OK;
     });
 }
 
 size_t block_bwd_workspace(int64_t n, int D) {
-    const int64_t most = n < kBwdWgs ? n : kBwdWgs;          // a workgroup takes a row at least
+    constexpr int kMost = kBlockWgs<RowTile<1, 64, 1>>;
+    const int64_t most = n < kMost ? n : kMost;              // a workgroup takes a row at least
     return sizeof(float) * (size_t)(most < 1 ? 1 : most) * kSums * D;
 }
 
 int launch_block_bwd(BlockBwd a, void* ws, hipStream_t s) {
+    if (!a.dN) {                  // nothing of the norm in front is read, so that nothing in it counts
+        a.X_out = nullptr;
+        a.saved.x = dr_act8{};
+    }
     const bool full = a.b.gate_cols == a.D;
-    const bool vector = vector_rows(a.D, {a.dX_out, a.dN, a.X_out, a.Y, full ? a.G : nullptr, a.grads.dX, a.grads.dY, full ? a.grads.dG : nullptr},
+    const bool floats = a.X_out || a.Y || (full && a.G), codes = a.saved.x.q || a.saved.y.q || a.saved.g.q;
+    // (some from tensors, some from checkpoints: the kernels of any width)
+    const bool vector = !(floats && codes) && vector_rows(a.D, {a.dX_out, a.dN, a.X_out, a.Y, full ? a.G : nullptr, a.grads.dX, a.grads.dY, full ? a.grads.dG : nullptr},
                                     {a.saved.x.q, a.saved.y.q, a.saved.g.q});
     a.part = static_cast<float*>(ws);
     a.parts = 0;
@@ -385,10 +378,19 @@ int launch_block_bwd(BlockBwd a, void* ws, hipStream_t s) {
         DRC_TRY(with_row_tile(a.D, vector, [&](auto tile) -> int {
             using T = decltype(tile);
             const int64_t blocks = (a.n + T::R - 1) / T::R;
-            a.parts = (int)(blocks < kBwdWgs ? blocks : kBwdWgs);
-            auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)a.parts), dim3(kRowThreads), 0, s, a); };
-            if (a.b.gate_cols) go(block_bwd_kernel<T, true>);
-            else go(block_bwd_kernel<T, false>);
+            a.parts = (int)(blocks < kBlockWgs<T> ? blocks : kBlockWgs<T>);
+            auto go = [&](auto gate) {
+                constexpr int GATE = decltype(gate)::value;
+                const dim3 grid((unsigned)a.parts);
+                if (!codes) {
+                    hipLaunchKernelGGL((block_bwd_kernel<T, GATE, kFloats>), grid, dim3(kRowThreads), 0, s, a);
+                } else if (!floats) {
+                    hipLaunchKernelGGL((block_bwd_kernel<T, GATE, kCodes>), grid, dim3(kRowThreads), 0, s, a);
+                } else if constexpr (T::W == 1) {
+                    hipLaunchKernelGGL((block_bwd_kernel<T, GATE, kEither>), grid, dim3(kRowThreads), 0, s, a);
+                }
+            };
+            by_gate(a.b.gate_cols, a.D, go);
             DRC_HIP(hipGetLastError());
             return DR_OK;
         }));
