@@ -1,6 +1,8 @@
 // 8-bit activation checkpoints: packing, unpacking, and weight gradients of projections whose input is held as one.
 #include "act8.h"
 
+#include <type_traits>
+
 namespace drc {
 
 template <typename T>
@@ -86,16 +88,21 @@ typedef double f64x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kGradWaves = 8, kGradThreads = 64 * kGradWaves;
-constexpr int kFlush = 4;                          // chunks that the matrix unit sums up by itself
+constexpr int kFlush = 8;                          // chunks that the matrix unit sums up by itself
 constexpr int kGradWgs = 256;                      // one workgroup per compute unit
 
-// TD x TF entries of dW; WA x WB wavefronts side by side on them, WK groups of those on 32 rows of a chunk each
+// TD x TF entries of dW; WA x WB wavefronts side by side on them, WK groups of those on 32 rows of a chunk each.  A wavefront's part is made of
+// 32 x 32 blocks where it is that wide: half as many matrix instructions as 16 x 16 ones take, each of which keeps vector instructions out
+// as long.
 template <int TD_, int TF_, int WA_, int WB_> struct GradTile {
     static constexpr int TD = TD_, TF = TF_, WA = WA_, WB = WB_, WK = kGradWaves / (WA * WB);
     static constexpr int CR = 32 * WK, RG = CR / 8;             // rows and units per column of a chunk
     static constexpr int AU = RG * TD, BU = RG * TF;            // units of A and of one part of dZ
     static constexpr int BUF = AU + 3 * BU;
-    static constexpr int MA = TD / (16 * WA), MB = TF / (16 * WB);      // 16 x 16 blocks per wavefront
+    static constexpr int M = TD / WA >= 32 && TF / WB >= 32 ? 32 : 16;  // width of a block
+    static constexpr int MA = TD / (M * WA), MB = TF / (M * WB);        // blocks per wavefront
+    static constexpr int KS = M / 16;                                   // matrix instructions per block, part and chunk
+    typedef float Block __attribute__((ext_vector_type(M * M / 64)));
     static_assert(AU <= kGradThreads && BU <= kGradThreads && AU % 64 == 0 && BU % 64 == 0 && MA >= 1 && MB >= 1);
 };
 
@@ -111,11 +118,9 @@ struct GradArgs {
 // the upper halves of a and b as two bf16 numbers
 __device__ __forceinline__ uint32_t upper2(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
-template <typename T> __device__ __forceinline__ void grad_walk_init(f32x4 (&c)[T::MA][T::MB]) {
-#pragma unroll
-    for (int i = 0; i < T::MA; ++i)
-#pragma unroll
-        for (int j = 0; j < T::MB; ++j) c[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+template <typename T> __device__ __forceinline__ typename T::Block grad_mfma(const bf16x8& b, const bf16x8& a, const typename T::Block& c) {
+    if constexpr (T::M == 32) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, a, c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, a, c, 0, 0, 0);
 }
 
 template <typename T> __global__ __launch_bounds__(kGradThreads, 2) void act8_wgrad_kernel(GradArgs a) {
@@ -126,35 +131,34 @@ template <typename T> __global__ __launch_bounds__(kGradThreads, 2) void act8_wg
     const int d0 = tile / a.tiles_f * T::TD, f0 = tile % a.tiles_f * T::TF;
     const int ca = d0 + tid % T::TD, ra = tid / T::TD * 8;      // this thread's units: column and first row of A, of dZ
     const int cb = f0 + tid % T::TF, rb = tid / T::TF * 8;
-    const bool has_a = wave * 64 < T::AU, has_b = wave * 64 < T::BU;    // whole wavefronts
+    const bool has_a = T::AU == kGradThreads || wave * 64 < T::AU, has_b = T::BU == kGradThreads || wave * 64 < T::BU;    // whole wavefronts
     const int D = a.D, F = a.F, G8 = a.groups * 8;
     const int at_a = ca < D ? ra * D + ca : kOutside, at_b = cb < F ? (rb * F + cb) * 4 : kOutside;
     const int at_s = ca < D ? (ra >> 3) * G8 + ca / kActGroup * 8 : kOutside;
     const int chunks = (int)((a.n + T::CR - 1) / T::CR);
 
-    uint32_t code[8];
-    u32x2 scales;
-    float y[8];
-    auto load = [&](int chunk) {                                // past the last chunk: reads nothing
+    struct Raw { uint32_t code[8]; u32x2 scales; float y[8]; } raw[2];
+    auto load = [&](int chunk, Raw& r) {                        // past the last chunk: reads nothing
         const int64_t base = (int64_t)chunk * T::CR;
         const int64_t left = a.n > base ? (a.n - base < T::CR ? a.n - base : T::CR) : 0;
         if (has_a) {
             const Buf q = buf_view(a.q + base * D, left * D), s = buf_view(a.scale + base / 8 * G8, (left + 7) / 8 * G8);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) code[j] = __builtin_amdgcn_raw_buffer_load_b8(q, at_a + j * D, 0, 0);
-            scales = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(s, at_s, 0, 0));
+            for (int j = 0; j < 8; ++j) r.code[j] = __builtin_amdgcn_raw_buffer_load_b8(q, at_a + j * D, 0, 0);
+            r.scales = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(s, at_s, 0, 0));
         }
         if (has_b) {
             const Buf b = buf_view(a.dZ + base * F, left * F * 4);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = of_bits(__builtin_amdgcn_raw_buffer_load_b32(b, at_b + j * F * 4, 0, 0));
+            for (int j = 0; j < 8; ++j) r.y[j] = of_bits(__builtin_amdgcn_raw_buffer_load_b32(b, at_b + j * F * 4, 0, 0));
         }
     };
-    auto commit = [&](int chunk, int to) {
+    auto commit = [&](int chunk, const Raw& r, int to) {
         bf16x8* const buf = smem + to * T::BUF;
         if (has_a) {
             // bytes of rows past the end may hold anything: they are zeros here
             const int64_t rows = a.n - ((int64_t)chunk * T::CR + ra);
+            u32x2 scales = r.scales;
             if (rows < 8) {
                 const uint64_t keep = rows <= 0 ? 0 : (uint64_t(1) << (8 * rows)) - 1;
                 scales[0] &= (uint32_t)keep;
@@ -165,7 +169,7 @@ template <typename T> __global__ __launch_bounds__(kGradThreads, 2) void act8_wg
             for (int j = 0; j < 8; ++j) {
                 // 255 << 23 is an infinity and the codes of such a group are zeros: not-a-numbers
                 const float f = of_bits(((scales[j >> 2] >> (8 * (j & 3))) & 255u) << 23);
-                v[j] = bits((float)(int8_t)code[j] * f);
+                v[j] = bits((float)(int8_t)r.code[j] * f);
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] = upper2(v[2 * j], v[2 * j + 1]);
@@ -176,16 +180,16 @@ template <typename T> __global__ __launch_bounds__(kGradThreads, 2) void act8_wg
             float most = 0.f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                most = fmaxf(most, fabsf(y[j]));
-                x1[j] = bits(y[j]);
-                const float r = y[j] - of_bits(x1[j] & 0xffff0000u);
-                x2[j] = bits(r);
-                x3[j] = bits(r - of_bits(x2[j] & 0xffff0000u));
+                most = fmaxf(most, fabsf(r.y[j]));
+                x1[j] = bits(r.y[j]);
+                const float rest = r.y[j] - of_bits(x1[j] & 0xffff0000u);
+                x2[j] = bits(rest);
+                x3[j] = bits(rest - of_bits(x2[j] & 0xffff0000u));
             }
             if (__builtin_amdgcn_ballot_w64(most == __builtin_inff())) {     // an infinity has no remainder
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (fabsf(y[j]) == __builtin_inff()) x2[j] = x3[j] = 0;
+                    if (fabsf(r.y[j]) == __builtin_inff()) x2[j] = x3[j] = 0;
             }
             auto put = [&](int part, const uint32_t (&x)[8]) {
                 uint32_t w[4];
@@ -199,52 +203,58 @@ template <typename T> __global__ __launch_bounds__(kGradThreads, 2) void act8_wg
         }
     };
 
-    f32x4 acc[T::MA][T::MB], hi[T::MA][T::MB], lo[T::MA][T::MB];
-    grad_walk_init<T>(acc);
-    grad_walk_init<T>(hi);
-    grad_walk_init<T>(lo);
+    using Block = typename T::Block;
+    Block acc[T::MA][T::MB] = {}, hi[T::MA][T::MB] = {}, lo[T::MA][T::MB] = {};
     const auto flush = [&]() {
 #pragma unroll
         for (int i = 0; i < T::MA; ++i)
 #pragma unroll
             for (int j = 0; j < T::MB; ++j) {
                 acc[i][j] += hi[i][j] + lo[i][j];
-                hi[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-                lo[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+                hi[i][j] = Block{};
+                lo[i][j] = Block{};
             }
     };
     const auto multiply = [&](int from) {
         const bf16x8* const buf = smem + from * T::BUF;
-        const int rg = 4 * wk + (lane >> 4), col = lane & 15;
-        bf16x8 fa[T::MA];
+        const int col = lane % T::M;
+        bf16x8 fa[T::MA][T::KS], fb[T::MB][3][T::KS];
 #pragma unroll
-        for (int i = 0; i < T::MA; ++i) fa[i] = buf[rg * T::TD + 16 * (wa * T::MA + i) + col];
+        for (int k = 0; k < T::KS; ++k) {
+            const int rg = 4 * wk + 4 / T::KS * k + lane / T::M;         // row group of this lane
 #pragma unroll
-        for (int j = 0; j < T::MB; ++j) {
-            bf16x8 fb[3];
+            for (int i = 0; i < T::MA; ++i) fa[i][k] = buf[rg * T::TD + T::M * (wa * T::MA + i) + col];
 #pragma unroll
-            for (int p = 0; p < 3; ++p) fb[p] = buf[T::AU + p * T::BU + rg * T::TF + 16 * (wb * T::MB + j) + col];
+            for (int j = 0; j < T::MB; ++j)
 #pragma unroll
-            for (int i = 0; i < T::MA; ++i) lo[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[2], fa[i], lo[i][j], 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < T::MA; ++i) lo[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[1], fa[i], lo[i][j], 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < T::MA; ++i) hi[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[0], fa[i], hi[i][j], 0, 0, 0);
+                for (int p = 2; p >= 0; --p) fb[j][p][k] = buf[T::AU + p * T::BU + rg * T::TF + T::M * (wb * T::MB + j) + col];
         }
+        __builtin_amdgcn_sched_barrier(0);
+        // consecutive instructions go to different sums
+#pragma unroll
+        for (int k = 0; k < T::KS; ++k)
+#pragma unroll
+            for (int j = 0; j < T::MB; ++j) {
+#pragma unroll
+                for (int i = 0; i < T::MA; ++i) lo[i][j] = grad_mfma<T>(fb[j][2][k], fa[i][k], lo[i][j]);
+#pragma unroll
+                for (int i = 0; i < T::MA; ++i) hi[i][j] = grad_mfma<T>(fb[j][0][k], fa[i][k], hi[i][j]);
+#pragma unroll
+                for (int i = 0; i < T::MA; ++i) lo[i][j] = grad_mfma<T>(fb[j][1][k], fa[i][k], lo[i][j]);
+            }
     };
-    const auto walk = [&](bool first) {
-        int chunk = z, cur = 0, since = 0;
-        if (chunk < chunks) {
-            load(chunk);
-            commit(chunk, 0);
-            load(chunk + a.splits);
-        }
-        for (; chunk < chunks; chunk += a.splits, cur ^= 1) {
+    // Two chunks are under way to the registers while one is in LDS and one is multiplied: 41 KB per compute unit (with one, 1.2 M x 128 x 128
+    // took 184 us).
+    const auto walk = [&](auto which) {
+        constexpr bool first = decltype(which)::value;
+        int chunk = z, since = 0;
+        const auto step = [&](auto at) {
+            constexpr int cur = decltype(at)::value;
             __syncthreads();                                    // this chunk is in LDS; the other buffer may be overwritten
             const int next = chunk + a.splits;
-            if (first) {
-                commit(next, cur ^ 1);
-                load(next + a.splits);
+            if constexpr (first) {
+                commit(next, raw[cur ^ 1], cur ^ 1);
+                load(next + 2 * a.splits, raw[cur ^ 1]);
             }
             __builtin_amdgcn_sched_barrier(0);
             multiply(cur);
@@ -253,22 +263,37 @@ template <typename T> __global__ __launch_bounds__(kGradThreads, 2) void act8_wg
                 since = 0;
             }
             __builtin_amdgcn_sched_barrier(0);
-            if (!first) {
-                commit(next, cur ^ 1);
-                load(next + a.splits);
+            if constexpr (!first) {
+                commit(next, raw[cur ^ 1], cur ^ 1);
+                load(next + 2 * a.splits, raw[cur ^ 1]);
             }
+            chunk = next;
+        };
+        if (chunk < chunks) {
+            load(chunk, raw[0]);
+            load(chunk + a.splits, raw[1]);
+            commit(chunk, raw[0], 0);
+            load(chunk + 2 * a.splits, raw[0]);
+        }
+        while (chunk < chunks) {
+            step(std::integral_constant<int, 0>{});
+            if (chunk >= chunks) break;
+            step(std::integral_constant<int, 1>{});
         }
         flush();
     };
-    if (wave < kGradWaves / 2) walk(true);
-    else walk(false);
-    // lane: row 16 i + (lane & 15) of the wavefront's part of the tile, columns 16 j + 4 (lane >> 4) ..
+    if (wave < kGradWaves / 2) walk(std::true_type{});
+    else walk(std::false_type{});
+    // lane: row lane % M of a block of the tile, four columns each from 4 (lane / M) on, every 8 columns (32 x 32; 16 x 16 has four in all)
     float* const out = a.part + ((size_t)blockIdx.x * T::WK + wk) * T::TD * T::TF;
 #pragma unroll
     for (int i = 0; i < T::MA; ++i)
 #pragma unroll
         for (int j = 0; j < T::MB; ++j)
-            *reinterpret_cast<f32x4*>(out + (size_t)(16 * (wa * T::MA + i) + (lane & 15)) * T::TF + 16 * (wb * T::MB + j) + 4 * (lane >> 4)) = acc[i][j];
+#pragma unroll
+            for (int r = 0; r < T::M * T::M / 64; r += 4)
+                *reinterpret_cast<f32x4*>(out + (size_t)(T::M * (wa * T::MA + i) + lane % T::M) * T::TF + T::M * (wb * T::MB + j) + 2 * r +
+                                          4 * (lane / T::M)) = f32x4{acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]};
 }
 
 // dW = the sum over a tile's partials: wavefront w of the workgroup sums partials w, w + 16, ... of 64 x 4 consecutive entries, then
