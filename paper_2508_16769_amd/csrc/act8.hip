@@ -88,7 +88,7 @@ typedef double f64x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kGradWaves = 8, kGradThreads = 64 * kGradWaves;
-constexpr int kFlush = 8;                          // chunks that the matrix unit sums up by itself
+constexpr int kFlush = 16;                          // chunks that the matrix unit sums up by itself
 constexpr int kGradWgs = 256;                      // one workgroup per compute unit
 
 // TD x TF entries of dW; WA x WB wavefronts side by side on them, WK groups of those on 32 rows of a chunk each.  A wavefront's part is made of
@@ -118,6 +118,23 @@ struct GradArgs {
 // the upper halves of a and b as two bf16 numbers
 __device__ __forceinline__ uint32_t upper2(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
+// byte N of w as an exponent: in bits 23 .. 30, zeros around it
+template <int N> __device__ __forceinline__ uint32_t byte_up(uint32_t w) {
+    uint32_t r;
+    const uint32_t by = 23;
+    if constexpr (N == 0) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_0" : "=v"(r) : "v"(by), "v"(w));
+    if constexpr (N == 1) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_1" : "=v"(r) : "v"(by), "v"(w));
+    if constexpr (N == 2) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_2" : "=v"(r) : "v"(by), "v"(w));
+    if constexpr (N == 3) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_3" : "=v"(r) : "v"(by), "v"(w));
+    return r;
+}
+template <int N, int I = 0, typename F> __device__ __forceinline__ void steps(F f) {       // f(0), ..., f(N - 1), each a constant
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        steps<N, I + 1>(f);
+    }
+}
+
 template <typename T> __device__ __forceinline__ typename T::Block grad_mfma(const bf16x8& b, const bf16x8& a, const typename T::Block& c) {
     if constexpr (T::M == 32) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, a, c, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, a, c, 0, 0, 0);
@@ -137,14 +154,14 @@ template <typename T> __global__ __launch_bounds__(kGradThreads, 2) void act8_wg
     const int at_s = ca < D ? (ra >> 3) * G8 + ca / kActGroup * 8 : kOutside;
     const int chunks = (int)((a.n + T::CR - 1) / T::CR);
 
-    struct Raw { uint32_t code[8]; u32x2 scales; float y[8]; } raw[2];
+    struct Raw { int code[8]; u32x2 scales; float y[8]; } raw[2];
     auto load = [&](int chunk, Raw& r) {                        // past the last chunk: reads nothing
         const int64_t base = (int64_t)chunk * T::CR;
         const int64_t left = a.n > base ? (a.n - base < T::CR ? a.n - base : T::CR) : 0;
         if (has_a) {
             const Buf q = buf_view(a.q + base * D, left * D), s = buf_view(a.scale + base / 8 * G8, (left + 7) / 8 * G8);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) r.code[j] = __builtin_amdgcn_raw_buffer_load_b8(q, at_a + j * D, 0, 0);
+            for (int j = 0; j < 8; ++j) r.code[j] = (int8_t)__builtin_amdgcn_raw_buffer_load_b8(q, at_a + j * D, 0, 0);
             r.scales = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(s, at_s, 0, 0));
         }
         if (has_b) {
@@ -157,20 +174,20 @@ template <typename T> __global__ __launch_bounds__(kGradThreads, 2) void act8_wg
         bf16x8* const buf = smem + to * T::BUF;
         if (has_a) {
             // bytes of rows past the end may hold anything: they are zeros here
-            const int64_t rows = a.n - ((int64_t)chunk * T::CR + ra);
             u32x2 scales = r.scales;
-            if (rows < 8) {
-                const uint64_t keep = rows <= 0 ? 0 : (uint64_t(1) << (8 * rows)) - 1;
+            const int64_t left = a.n - (int64_t)chunk * T::CR;
+            if (left < T::CR) {
+                const int rows = (int)left - ra;
+                const uint64_t keep = rows <= 0 ? 0 : rows >= 8 ? ~uint64_t(0) : (uint64_t(1) << (8 * rows)) - 1;
                 scales[0] &= (uint32_t)keep;
                 scales[1] &= (uint32_t)(keep >> 32);
             }
             uint32_t v[8], w[4];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                // 255 << 23 is an infinity and the codes of such a group are zeros: not-a-numbers
-                const float f = of_bits(((scales[j >> 2] >> (8 * (j & 3))) & 255u) << 23);
-                v[j] = bits((float)(int8_t)r.code[j] * f);
-            }
+            // 255 << 23 is an infinity and the codes of such a group are zeros: not-a-numbers
+            steps<8>([&](auto at) {
+                constexpr int j = decltype(at)::value;
+                v[j] = bits((float)r.code[j] * of_bits(byte_up<j % 4>(scales[j / 4])));
+            });
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] = upper2(v[2 * j], v[2 * j + 1]);
             buf[tid] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
