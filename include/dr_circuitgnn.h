@@ -375,6 +375,35 @@ int heteroconv_bwd(dr_heteroconv* ctx, const float* dY_cell, const float* dY_net
                    const dr_heteroconv_weights* W, const dr_heteroconv_saved* saved,
                    float* dX_cell, float* dX_net, const dr_heteroconv_wgrads* dW, void* stream);
 
+/*
+ * The layer with its messages kept in 8 bits: H_near, H_pins and H_pinned, of all that a forward pass leaves the largest part, are left as
+ * checkpoints (dr_act8) and read from them by the weight gradients of the backward pass.  Y_cell, Y_net and the other saved
+ * buffers are what heteroconv_fwd writes, bit for bit; so are dX_cell and dX_net of the backward pass.  The weight gradients of the
+ * messages are those at the values that the checkpoints stand for, those of the self terms the same up to the order of their sums.  While a
+ * forward pass runs, its messages lie in the context's scratch:
+ * like backward passes, forward passes of this kind follow one another on whatever streams they are called.
+ */
+typedef struct dr_heteroconv_saved8 {         /* as dr_heteroconv_saved, the messages as checkpoints */
+    float*    vals_cell;
+    uint16_t* idx_cell;
+    float*    vals_net;
+    uint16_t* idx_net;
+    dr_act8   H_near;     /* of [Nc,D] */
+    dr_act8   H_pins;     /* of [Nn,D] */
+    dr_act8   H_pinned;   /* of [Nc,D] */
+    uint8_t*  mask;
+    float*    vals_cell_pins;
+    uint16_t* idx_cell_pins;
+    float*    vals_net_self;
+    uint16_t* idx_net_self;
+} dr_heteroconv_saved8;
+int heteroconv_fwd_act8(dr_heteroconv* ctx, const float* X_cell, const float* X_net,
+                        const dr_heteroconv_weights* W, float* Y_cell, float* Y_net,
+                        const dr_heteroconv_saved8* saved, void* stream);
+int heteroconv_bwd_act8(dr_heteroconv* ctx, const float* dY_cell, const float* dY_net,
+                        const dr_heteroconv_weights* W, const dr_heteroconv_saved8* saved,
+                        float* dX_cell, float* dX_net, const dr_heteroconv_wgrads* dW, void* stream);
+
 /* Transposed adjacency of a relation held by the context (which: 0 near, 1 pins, 2 pinned); the
  * returned struct's pointers are device memory owned by the context. */
 int heteroconv_get_transpose(const dr_heteroconv* ctx, int which, dr_csr* out);

@@ -39,7 +39,7 @@ EXPORTS = (
     "dr_block_fwd", "dr_block_bwd_workspace_bytes", "dr_block_bwd",
     "dr_csr_transpose_workspace_bytes", "dr_csr_transpose",
     "dr_csr_normalize_workspace_bytes", "dr_csr_normalize", "dr_csr_normalize_noalloc",
-    "heteroconv_create", "heteroconv_create_per_relation", "heteroconv_get_k", "heteroconv_profile_k", "heteroconv_fwd", "heteroconv_bwd", "heteroconv_get_transpose", "heteroconv_destroy",
+    "heteroconv_create", "heteroconv_create_per_relation", "heteroconv_get_k", "heteroconv_profile_k", "heteroconv_fwd", "heteroconv_bwd", "heteroconv_fwd_act8", "heteroconv_bwd_act8", "heteroconv_get_transpose", "heteroconv_destroy",
     "heteroconv_profile", "heteroconv_num_kernels", "heteroconv_kernel_name", "heteroconv_kernel_times",
     "heteroconv_set_overlap", "heteroconv_set_cell_order",
     "dr_pipeline_create", "dr_pipeline_submit", "dr_pipeline_acquire", "dr_pipeline_relations", "dr_pipeline_release",
@@ -121,6 +121,13 @@ class dr_block_saved(ctypes.Structure):
 
 class dr_block_grads(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("dX", "dY", "dG", "dw_after", "db_after", "dscale", "dw_before", "db_before")]
+
+
+class dr_heteroconv_saved8(ctypes.Structure):
+    _fields_ = [("vals_cell", ctypes.c_void_p), ("idx_cell", ctypes.c_void_p), ("vals_net", ctypes.c_void_p), ("idx_net", ctypes.c_void_p),
+                ("H_near", dr_act8), ("H_pins", dr_act8), ("H_pinned", dr_act8), ("mask", ctypes.c_void_p),
+                ("vals_cell_pins", ctypes.c_void_p), ("idx_cell_pins", ctypes.c_void_p), ("vals_net_self", ctypes.c_void_p),
+                ("idx_net_self", ctypes.c_void_p)]
 
 
 def _declare_row_operators(lib) -> None:
@@ -457,6 +464,27 @@ class HeteroConv:
         w, s, g = self._weights(W), self._saved(saved), self._weights(dW)
         _check(load().heteroconv_bwd(self._ctx, _ptr(dY_cell), _ptr(dY_net), ctypes.byref(w), ctypes.byref(s),
                                      _ptr(dX_cell), _ptr(dX_net), ctypes.byref(g), _stream(stream)))
+
+    def alloc_saved8(self, device="cuda") -> dict:
+        """As alloc_saved, with the messages H_near, H_pins and H_pinned as checkpoints (pairs (q, scale))."""
+        out = {n: t for n, t in self.alloc_saved(device).items() if not n.startswith("H_")}
+        return dict(out, H_near=alloc_act8(self.Nc, self.D, device), H_pins=alloc_act8(self.Nn, self.D, device),
+                    H_pinned=alloc_act8(self.Nc, self.D, device))
+
+    @staticmethod
+    def _saved8(saved: dict) -> dr_heteroconv_saved8:
+        return dr_heteroconv_saved8(*[_act8(saved[n]) if n.startswith("H_") else _address(saved.get(n))
+                                      for n, _ in dr_heteroconv_saved8._fields_])
+
+    def heteroconv_fwd_act8(self, X_cell, X_net, W, Y_cell, Y_net, saved8, stream=None) -> None:
+        w, s = self._weights(W), self._saved8(saved8)
+        _check(load().heteroconv_fwd_act8(self._ctx, _ptr(X_cell), _ptr(X_net), ctypes.byref(w), _ptr(Y_cell), _ptr(Y_net),
+                                          ctypes.byref(s), _stream(stream)))
+
+    def heteroconv_bwd_act8(self, dY_cell, dY_net, W, saved8, dX_cell, dX_net, dW, stream=None) -> None:
+        w, s, g = self._weights(W), self._saved8(saved8), self._weights(dW)
+        _check(load().heteroconv_bwd_act8(self._ctx, _ptr(dY_cell), _ptr(dY_net), ctypes.byref(w), ctypes.byref(s), _ptr(dX_cell),
+                                          _ptr(dX_net), ctypes.byref(g), _stream(stream)))
 
     def heteroconv_get_transpose(self, which: int) -> dr_csr:
         out = dr_csr()

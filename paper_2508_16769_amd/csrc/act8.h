@@ -6,7 +6,6 @@
 namespace drc {
 
 constexpr int kActGroup = DR_ACT8_GROUP;
-__host__ __device__ inline int act_groups(int D) { return (D + kActGroup - 1) / kActGroup; }
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -231,32 +230,5 @@ template <typename F> int with_row_tile(int D, bool vector, F f) {
     if (D <= 512) return f(RowTile<1, 128, 4>{});
     return f(RowTile<1, 256, 4>{});
 }
-
-// host side ------------------------------------------------------------------------------------------
-int launch_act8_pack(const float* X, int64_t n, int D, const dr_act8& out, hipStream_t s);
-int launch_act8_unpack(const dr_act8& in, int64_t n, int D, float* X, hipStream_t s);
-size_t act8_wgrad_workspace(int64_t n, int D, int F);
-int launch_act8_wgrad(const dr_act8& A, int64_t n, int D, const float* dZ, int F, float* dW, bool accumulate, void* ws, hipStream_t s);
-struct BlockFwd {
-    dr_block b;
-    int64_t n;
-    int D;
-    const float *X, *Y, *G;
-    float *X_out, *N;
-    dr_block_saved saved;
-};
-int launch_block_fwd(const BlockFwd& a, hipStream_t s);
-struct BlockBwd {
-    dr_block b;
-    int64_t n;
-    int D;
-    const float *dX_out, *dN, *X_out, *Y, *G;
-    dr_block_saved saved;
-    dr_block_grads grads;
-    float* part;                  // [workgroups][5][D]
-    int parts;
-};
-size_t block_bwd_workspace(int64_t n, int D);
-int launch_block_bwd(BlockBwd a, void* ws, hipStream_t s);
 
 }  // namespace drc

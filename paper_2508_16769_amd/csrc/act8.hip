@@ -5,19 +5,28 @@
 
 namespace drc {
 
-template <typename T>
-__global__ __launch_bounds__(kRowThreads) void act8_pack_kernel(const float* X, int64_t n, int D, int8_t* q, uint8_t* scale) {
+// Matrices of one width, each a range of the workgroups.
+struct PackArgs {
+    Act8Pack m[kMaxPacks];
+    int first[kMaxPacks + 1];     // workgroup
+    int D;
+};
+template <typename T> __global__ __launch_bounds__(kRowThreads) void act8_pack_kernel(PackArgs a) {
+    const int D = a.D, groups = act_groups(D);
     const RowLane<T> l(D);
-    const int groups = act_groups(D);
-    const int64_t n8 = (n + 7) & ~int64_t(7);                   // the rows that fill up the last eight have scale bytes
-    for (int64_t r0 = (int64_t)blockIdx.x * T::R; r0 < n8; r0 += (int64_t)gridDim.x * T::R) {
-        const int left = (int)(n - r0 < T::R ? (n > r0 ? n - r0 : 0) : T::R);
+    int i = 0;
+    while (i + 1 < kMaxPacks && (int)blockIdx.x >= a.first[i + 1]) ++i;
+    const Act8Pack m = a.m[i];
+    const int64_t n8 = (m.n + 7) & ~int64_t(7);                 // the rows that fill up the last eight have scale bytes
+    const int64_t step = (int64_t)(a.first[i + 1] - a.first[i]) * T::R;
+    for (int64_t r0 = (int64_t)((int)blockIdx.x - a.first[i]) * T::R; r0 < n8; r0 += step) {
+        const int left = (int)(m.n - r0 < T::R ? (m.n > r0 ? m.n - r0 : 0) : T::R);
         uint32_t raw[T::E];
         float x[T::E];
-        load_rows<T>(rows_view(X, r0, left, 4 * D), l, raw);
+        load_rows<T>(rows_view(m.X, r0, left, 4 * D), l, raw);
 #pragma unroll
-        for (int i = 0; i < T::E; ++i) x[i] = of_bits(raw[i]);
-        store_codes<T>(rows_view(q, r0, left, D), scales_view(scale, r0, n, groups), l, l.row < left, x);
+        for (int e = 0; e < T::E; ++e) x[e] = of_bits(raw[e]);
+        store_codes<T>(rows_view(m.out.q, r0, left, D), scales_view(m.out.scale, r0, m.n, groups), l, l.row < left, x);
     }
 }
 
@@ -46,13 +55,30 @@ static unsigned row_blocks(int64_t rows, int rows_per_block) {
 // (1.2 M x 128 packed and unpacked 294 / 272 us).
 constexpr int64_t kStreamFrom = int64_t(1) << 26;
 
-int launch_act8_pack(const float* X, int64_t n, int D, const dr_act8& out, hipStream_t s) {
-    return with_row_tile(D, D % 4 == 0 && aligned(X, 16) && aligned(out.q, 4), [&](auto tile) -> int {
+int launch_act8_packs(const Act8Pack* jobs, int n, int D, hipStream_t s) {
+    bool vector = D % 4 == 0;
+    for (int i = 0; i < n; ++i) vector = vector && aligned(jobs[i].X, 16) && aligned(jobs[i].out.q, 4);
+    return with_row_tile(D, vector, [&](auto tile) -> int {
         using T = decltype(tile);
-        hipLaunchKernelGGL((act8_pack_kernel<T>), dim3(row_blocks((n + 7) / 8 * 8, T::R)), dim3(kRowThreads), 0, s, X, n, D, out.q, out.scale);
+        PackArgs a{};
+        a.D = D;
+        unsigned blocks = 0;
+        for (int i = 0; i < kMaxPacks; ++i) {
+            a.first[i] = (int)blocks;
+            if (i >= n) continue;
+            a.m[i] = jobs[i];
+            blocks += row_blocks((jobs[i].n + 7) / 8 * 8, T::R);
+        }
+        a.first[kMaxPacks] = (int)blocks;
+        if (blocks == 0) return DR_OK;
+        hipLaunchKernelGGL((act8_pack_kernel<T>), dim3(blocks), dim3(kRowThreads), 0, s, a);
         DRC_HIP(hipGetLastError());
         return DR_OK;
     });
+}
+int launch_act8_pack(const float* X, int64_t n, int D, const dr_act8& out, hipStream_t s) {
+    const Act8Pack job{X, n, out};
+    return launch_act8_packs(&job, 1, D, s);
 }
 
 int launch_act8_unpack(const dr_act8& in, int64_t n, int D, float* X, hipStream_t s) {

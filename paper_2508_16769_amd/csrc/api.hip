@@ -1,5 +1,5 @@
 // C ABI entry points: host-side argument validation, then the kernel launchers.
-#include "act8.h"
+#include "dr_internal.h"
 
 #include <cstring>
 

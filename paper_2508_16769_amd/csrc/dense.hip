@@ -763,6 +763,24 @@ template <int D> struct WTile {
     static_assert(KG == T::RG && CR * TPR <= T::THREADS, "chunk shape");
 };
 
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+// Eight codes of a column, rows side by side, with their scale bytes; `left` rows are there.  A scale byte of 255 is an infinity here, and the codes
+// of such a group are zeros: not-a-numbers.
+__device__ __forceinline__ void decode8(const int (&q)[8], const u32x2& f, int left, float (&x)[8]) {
+    const uint64_t keep = left >= 8 ? ~uint64_t(0) : left <= 0 ? 0 : (uint64_t(1) << (8 * left)) - 1;
+    const uint32_t w[2] = {f[0] & (uint32_t)keep, f[1] & (uint32_t)(keep >> 32)};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = (float)q[j] * __builtin_bit_cast(float, ((w[j / 4] >> (8 * (j % 4))) & 255u) << 23);
+}
+// half of each of eight numbers that bf16 holds exactly
+__device__ __forceinline__ bf16x8 exact8(const float (&x)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = pack2(kScale * x[2 * j], kScale * x[2 * j + 1]);
+    struct Words { uint32_t w[4]; };
+    return __builtin_bit_cast(bf16x8, Words{w[0], w[1], w[2], w[3]});
+}
+
 struct WgradSeg {                 // one side of one graph
     const float *dY, *H1, *H2, *vals;     // H2, mask: cells only
     const uint8_t* mask;
@@ -801,8 +819,18 @@ __device__ __forceinline__ f32x4 cut_to_finite(const f32x4& x) {
     return v;
 }
 
-template <int D, bool CELL>
-__device__ __forceinline__ void wgrad_side(const DRC_CONST WgradSeg* g, bf16x8* smem, int wg) {
+// Messages kept in 8 bits (ACT8): H1 and H2 are codes, and what a code stands for is one bf16 number, so that a product with it takes three
+// bf16 products instead of six.
+struct Wgrad8Seg {
+    WgradSeg s;
+    const uint8_t *scale1, *scale2;
+};
+__device__ __forceinline__ const DRC_CONST WgradSeg* plain(const DRC_CONST WgradSeg* g) { return g; }
+__device__ __forceinline__ const DRC_CONST WgradSeg* plain(const DRC_CONST Wgrad8Seg* g) { return &g->s; }
+
+template <int D, bool CELL, bool ACT8 = false, typename SEG>
+__device__ __forceinline__ void wgrad_side(const DRC_CONST SEG* seg, bf16x8* smem, int wg) {
+    const DRC_CONST WgradSeg* const g = plain(seg);
     using T = Tile<D>;
     using W = WTile<D>;
     constexpr int NP = CELL ? 3 : 2;
@@ -834,8 +862,23 @@ __device__ __forceinline__ void wgrad_side(const DRC_CONST WgradSeg* g, bf16x8* 
         load_pairs<W::TPR>(pr, block_view(g->vals + (size_t)base * g->k, left, g->k * 4), block_view(g->idx + (size_t)base * g->k, left, g->k * 2),
                            g->k, prow, ppart);
     };
+    constexpr int G8 = 8 * (D / 32);               // scale bytes of eight rows
+    int q1[8], q2[8];                              // codes and, for eight rows side by side, scale bytes
+    u32x2 f1, f2;
     auto load_h = [&](int chunk) {
         const int base = chunk * W::CR, left = g->rows - base;
+        if constexpr (ACT8) {
+            const auto load_codes = [&](const float* H, const uint8_t* scale, int (&q)[8], u32x2& f) {
+                const Buf b = block_view(reinterpret_cast<const int8_t*>(H) + (size_t)base * D, left, D);
+                const Buf bs = block_view(scale + (size_t)(base >> 3) * G8, (left + 7) >> 3, G8);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) q[j] = (int8_t)__builtin_amdgcn_raw_buffer_load_b8(b, (hoff >> 2) + j * D, 0, kNt);
+                f = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(bs, (hrow >> 3) * G8 + (hcol >> 5) * 8, 0, kNt));
+            };
+            load_codes(g->H1, seg->scale1, q1, f1);
+            if constexpr (CELL) load_codes(g->H2, seg->scale2, q2, f2);
+            return;
+        }
         const Buf b1 = block_view(g->H1 + (size_t)base * D, left, D * 4);
         const Buf b2 = block_view(g->H2 + (size_t)base * D, left, D * 4);
 #pragma unroll
@@ -923,11 +966,21 @@ __device__ __forceinline__ void wgrad_side(const DRC_CONST WgradSeg* g, bf16x8* 
             };
             if constexpr (kFirst) stage_next();
             __builtin_amdgcn_sched_barrier(0);
+            if constexpr (ACT8) {
+                const int left = g->rows - chunk * W::CR - hrow;         // scale bytes of rows past the end may hold anything
+                decode8(q1, f1, left, h1);
+                if constexpr (CELL) decode8(q2, f2, left, h2);
+            }
             float most = largest(h1);
             if constexpr (CELL) most = largest(h2, most);
-            const Split8 a1 = split8(h1);
-            Split8 a2;
-            if constexpr (CELL) a2 = split8(h2);
+            Split8 a1, a2;
+            if constexpr (ACT8) {
+                a1.p[0] = exact8(h1);
+                if constexpr (CELL) a2.p[0] = exact8(h2);
+            } else {
+                a1 = split8(h1);
+                if constexpr (CELL) a2 = split8(h2);
+            }
             // H is a wavefront's own, what is staged is everybody's
             const bool cut = __builtin_amdgcn_readfirstlane(wide[cur]) == chunk || __builtin_amdgcn_ballot_w64(most >= kWide) != 0;
             __builtin_amdgcn_sched_barrier(0);
@@ -951,9 +1004,10 @@ __device__ __forceinline__ void wgrad_side(const DRC_CONST WgradSeg* g, bf16x8* 
                 }
 #pragma unroll
                 for (int i = 0; i < 5; ++i) {
-                    lo[0] = mfma(b[BW[i]], a1.p[AW[i]], lo[0]);
+                    if (!ACT8 || AW[i] == 0) lo[0] = mfma(b[BW[i]], a1.p[ACT8 ? 0 : AW[i]], lo[0]);
                     lo[1] = mfma(b[BW[i]], aS[AW[i]], lo[1]);
-                    if constexpr (CELL) lo[2] = mfma(b2[BW[i]], a2.p[AW[i]], lo[2]);
+                    if constexpr (CELL)
+                        if (!ACT8 || AW[i] == 0) lo[2] = mfma(b2[BW[i]], a2.p[ACT8 ? 0 : AW[i]], lo[2]);
                 }
                 const f32x4 zero = {};
                 f32x4 hi[3];
@@ -1006,6 +1060,18 @@ template <int D>
 __global__ __launch_bounds__(Tile<D>::THREADS, 2) void wgrad_partial_kernel(WgradArgs<kMaxGraphs> a) {
     extern __shared__ bf16x8 smem8[];
     wgrad_workgroup<D>(kernel_args<WgradArgs<kMaxGraphs>>(), smem8, blockIdx.x);
+}
+
+// One graph's weight gradients from messages kept in 8 bits: the cells' workgroups, then the nets'.
+struct Wgrad8Args { Wgrad8Seg s[2]; int n; };
+template <int D>
+__global__ __launch_bounds__(Tile<D>::THREADS, 2) void saved8_wgrad_kernel(Wgrad8Args a) {
+    extern __shared__ bf16x8 smem8[];
+    const DRC_CONST Wgrad8Args* const k = kernel_args<Wgrad8Args>();
+    const DRC_CONST Wgrad8Seg* const g = k->s + (k->n > 1 && (int)blockIdx.x >= k->s[1].s.wg0 ? 1 : 0);
+    const int wg = (int)blockIdx.x - g->s.wg0;
+    if (g->s.mask) wgrad_side<D, true, true>(g, smem8, wg);
+    else wgrad_side<D, false, true>(g, smem8, wg);
 }
 
 // Weight gradients and projections of a backward pass in one launch.  Neither waits for the other, and while either has fewer tiles
@@ -1255,6 +1321,39 @@ static int launch_wgrads_to(const WgradJob* jobs, int n, int D, PartialSum* tabl
     }
 }
 int launch_wgrads(const WgradJob* jobs, int n, int D, hipStream_t s) { return launch_wgrads_to(jobs, n, D, nullptr, s); }
+
+template <int D> static int launch_wgrads8_d(WgradArgs<kMaxGraphs>& a, const Wgrad8Job* jobs, hipStream_t s) {
+    using T = Tile<D>;
+    static PerDevice cache;
+    int res = 0;
+    DRC_TRY(resident(&saved8_wgrad_kernel<D>, T::THREADS, wgrad_lds<D>(), cache, &res));
+    const int wgs = plan_wgrad<D>(a, res);
+    Wgrad8Args b{};
+    b.n = a.n;
+    for (int i = 0; i < a.n; ++i) b.s[i] = Wgrad8Seg{a.s[i], jobs[i].H1.scale, jobs[i].H2.scale};
+    hipLaunchKernelGGL((saved8_wgrad_kernel<D>), dim3((unsigned)wgs), dim3(T::THREADS), wgrad_lds<D>(), s, b);
+    hipLaunchKernelGGL((wgrad_reduce_kernel<D>), dim3((unsigned)(a.n * 3 * (D * D / 256))), dim3(64 * kRedWaves), 0, s, a);
+    DRC_HIP(hipGetLastError());
+    return DR_OK;
+}
+int launch_wgrads8(const Wgrad8Job* jobs, int n, int D, hipStream_t s) {
+    if (n < 1 || n > 2) return fail(DR_ERR_INVALID_ARG, "weight gradients of %d operands from checkpoints", n);
+    WgradJob plain[2];
+    for (int i = 0; i < n; ++i) {
+        plain[i] = jobs[i].job;
+        plain[i].H1 = reinterpret_cast<const float*>(jobs[i].H1.q);
+        plain[i].H2 = reinterpret_cast<const float*>(jobs[i].H2.q);
+    }
+    WgradArgs<kMaxGraphs> a{};
+    set_wgrad(a, plain, n);
+    switch (D) {
+        case 32: return launch_wgrads8_d<32>(a, jobs, s);
+        case 64: return launch_wgrads8_d<64>(a, jobs, s);
+        case 96: return launch_wgrads8_d<96>(a, jobs, s);
+        case 128: return launch_wgrads8_d<128>(a, jobs, s);
+        default: return fail(DR_ERR_UNSUPPORTED, "projection width D = %d not in {32,64,96,128}", D);
+    }
+}
 
 template <int D> static int launch_dense_bwd_d(const WgradJob* wgrads, const ProjBwdJob* proj, int n, const dr_heteroconv_weights& W,
                                                PartialSum* table, hipStream_t s) {

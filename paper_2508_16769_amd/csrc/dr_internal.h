@@ -187,6 +187,7 @@ struct BackwardOptions {
     bool gate_inputs = false;     // zero dX where the layer's input was not positive (ReLU in front of the layer)
     bool skip_dx = false;         // weight gradients only: dX_cell / dX_net are not written (and may be null)
     bool dy_net_zero = false;     // dY_net is all zeros: what it would feed is not computed (fills instead)
+    const dr_heteroconv_saved8* saved8 = nullptr;     // one graph: its messages are the checkpoints of this instead of S's
 };
 struct LayerBwd {
     dr_heteroconv* c;
@@ -248,11 +249,52 @@ struct WgradJob {                 // one node type of one graph; with a mask: ce
 };
 size_t wgrad_scratch_bytes(int64_t rows, int D, int products);
 int launch_wgrads(const WgradJob* jobs, int n, int D, hipStream_t s);      // n <= 2 * kMaxGraphs
+struct Wgrad8Job {                // the same with messages that were kept in 8 bits: H1, H2 of `job` are not read
+    WgradJob job;
+    dr_act8 H1, H2;
+};
+int launch_wgrads8(const Wgrad8Job* jobs, int n, int D, hipStream_t s);    // n <= 2
 // Weight gradients (cells and nets of each graph in turn) and projections of a backward pass.  The partial sums of the weight gradients
 // are left to launch_spmm_dense, or to launch_pending_sums; `table` has room for kSumsPerGraph entries a graph.
 constexpr int kSumsPerGraph = 5;
 int launch_dense_bwd(const WgradJob* wgrads, const ProjBwdJob* proj, int n, const dr_heteroconv_weights& W, int D, PartialSum* table,
                      PendingSums* pending, hipStream_t s);
 int launch_pending_sums(const PendingSums& pending, hipStream_t s);
+
+// 8-bit activation checkpoints and residual blocks -----------------------------------------------------
+__host__ __device__ inline int act_groups(int D) { return (D + DR_ACT8_GROUP - 1) / DR_ACT8_GROUP; }
+constexpr int kMaxPacks = 3;      // matrices per launch
+struct Act8Pack {
+    const float* X;
+    int64_t n;
+    dr_act8 out;
+};
+int launch_act8_packs(const Act8Pack* jobs, int n, int D, hipStream_t s);        // n <= kMaxPacks
+int launch_act8_pack(const float* X, int64_t n, int D, const dr_act8& out, hipStream_t s);
+int launch_act8_unpack(const dr_act8& in, int64_t n, int D, float* X, hipStream_t s);
+size_t act8_wgrad_workspace(int64_t n, int D, int F);
+int launch_act8_wgrad(const dr_act8& A, int64_t n, int D, const float* dZ, int F, float* dW, bool accumulate, void* ws, hipStream_t s);
+struct BlockFwd {
+    dr_block b;
+    int64_t n;
+    int D;
+    const float *X, *Y, *G;
+    float *X_out, *N;
+    dr_block_saved saved;
+};
+int launch_block_fwd(const BlockFwd& a, hipStream_t s);
+struct BlockBwd {
+    dr_block b;
+    int64_t n;
+    int D;
+    const float *dX_out, *dN, *X_out, *Y, *G;
+    dr_block_saved saved;
+    dr_block_grads grads;
+    float* part;                  // [workgroups][5][D]
+    int parts;
+};
+size_t block_bwd_workspace(int64_t n, int D);
+int launch_block_bwd(BlockBwd a, void* ws, hipStream_t s);
+
 
 }  // namespace drc

@@ -10,6 +10,7 @@
 // of a context that is called on another stream than the one before it (the scratch is the context's).
 #include "dr_internal.h"
 
+#include <initializer_list>
 #include <new>
 #include <vector>
 
@@ -647,11 +648,21 @@ static int backward_pass(const LayerBwd* g, int n, const dr_heteroconv_weights* 
         if (q.net_split && !net_zero) jn.more[0] = CompactPiece{q.i_self, c->k_self, c->S_net, g_self};
     }
     const bool alone = apart && n == 1;
+    Wgrad8Job w8[2] = {};
+    if (const dr_heteroconv_saved8* const q = opt.saved8) {
+        w8[0] = Wgrad8Job{wj[0], q->H_near, q->H_pinned};
+        w8[1] = Wgrad8Job{wj[1], q->H_pins, dr_act8{}};
+    }
     // The weight gradients come first: what the projections write is then gathered right away.
     if (!alone) {
         if (!need_dx) return launch_wgrads(wj, 2 * n, D, s);
         PendingSums sums{};
-        DRC_TRY(launch_dense_bwd(wj, pj, n, *W, D, g[0].c->wg_sums, &sums, s));
+        if (opt.saved8) {
+            DRC_TRY(launch_wgrads8(w8, 2, D, s));
+            DRC_TRY(launch_proj_bwd(pj, n, *W, D, s));
+        } else {
+            DRC_TRY(launch_dense_bwd(wj, pj, n, *W, D, g[0].c->wg_sums, &sums, s));
+        }
         for (int i = 0; i < n; ++i)
             if (g[i].c->near_plan)
                 DRC_TRY(launch_spmm_bwd_planned(g[i].c->near_plan, g[i].c->dH, cbsr_sets(g[i].c, g[i].S).i_near, g[i].c->k_near, g[i].c->S_cell, 1, s));
@@ -661,8 +672,8 @@ static int backward_pass(const LayerBwd* g, int n, const dr_heteroconv_weights* 
         return launch_pending_sums(sums, s);
     }
     dr_heteroconv* c = g[0].c;
-    { ScopedTiming tm(c, kWgCell, s); DRC_TRY(launch_wgrads(&wj[0], 1, D, s)); }
-    { ScopedTiming tm(c, kWgPins, s); DRC_TRY(launch_wgrads(&wj[1], 1, D, s)); }
+    { ScopedTiming tm(c, kWgCell, s); DRC_TRY(opt.saved8 ? launch_wgrads8(&w8[0], 1, D, s) : launch_wgrads(&wj[0], 1, D, s)); }
+    { ScopedTiming tm(c, kWgPins, s); DRC_TRY(opt.saved8 ? launch_wgrads8(&w8[1], 1, D, s) : launch_wgrads(&wj[1], 1, D, s)); }
     if (!need_dx) return DR_OK;
     ProjBwdJob part = pj[0];
     part.Nc = 0;
@@ -690,30 +701,84 @@ void drc::heteroconv_hand_over(dr_heteroconv* c, hipStream_t from, hipStream_t t
     if (!c->has_last || c->last_stream == from) heteroconv_ordered_on(c, to);
 }
 
-int drc::heteroconv_backward(const LayerBwd* g, int n, const dr_heteroconv_weights* W, hipStream_t s, BackwardOptions opt) {
+// A pass that uses the scratch of n contexts, ordered behind the passes that used it before on other streams.
+template <typename F> static int in_scratch(dr_heteroconv* const* c, int n, hipStream_t s, F pass) {
     bool plain = true;
-    for (int i = 0; i < n; ++i) plain = plain && (!g[i].c || (g[i].c->has_last && g[i].c->last_stream == s && !g[i].c->many_streams));
-    if (plain) return backward_pass(g, n, W, s, opt);
+    for (int i = 0; i < n; ++i) plain = plain && (!c[i] || (c[i]->has_last && c[i]->last_stream == s && !c[i]->many_streams));
+    if (plain) return pass();
     // A captured pass is ordered by the graph it becomes part of: events of the world outside do not belong in it.
     hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
     DRC_HIP(hipStreamIsCapturing(s, &capture));
-    if (capture != hipStreamCaptureStatusNone) return backward_pass(g, n, W, s, opt);
+    if (capture != hipStreamCaptureStatusNone) return pass();
     for (int i = 0; i < n; ++i) {
-        dr_heteroconv* const c = g[i].c;
-        if (!c) continue;
-        if (c->has_last && c->last_stream != s) {
-            if (c->end_recorded) DRC_HIP(hipStreamWaitEvent(s, c->end, 0));
+        if (!c[i]) continue;
+        if (c[i]->has_last && c[i]->last_stream != s) {
+            if (c[i]->end_recorded) DRC_HIP(hipStreamWaitEvent(s, c[i]->end, 0));
             else DRC_HIP(hipDeviceSynchronize());
-            c->many_streams = true;
+            c[i]->many_streams = true;
         }
-        heteroconv_ordered_on(c, s);
-        c->end_recorded = false;
+        heteroconv_ordered_on(c[i], s);
+        c[i]->end_recorded = false;
     }
-    DRC_TRY(backward_pass(g, n, W, s, opt));
+    DRC_TRY(pass());
     for (int i = 0; i < n; ++i)
-        if (g[i].c->many_streams) {
-            DRC_HIP(hipEventRecord(g[i].c->end, s));
-            g[i].c->end_recorded = true;
+        if (c[i]->many_streams) {
+            DRC_HIP(hipEventRecord(c[i]->end, s));
+            c[i]->end_recorded = true;
         }
     return DR_OK;
 }
+
+int drc::heteroconv_backward(const LayerBwd* g, int n, const dr_heteroconv_weights* W, hipStream_t s, BackwardOptions opt) {
+    DRC_REQUIRE(n >= 1 && n <= kMaxGraphs, "heteroconv_bwd: %d graphs in one pass", n);
+    dr_heteroconv* c[kMaxGraphs];
+    for (int i = 0; i < n; ++i) c[i] = g[i].c;
+    return in_scratch(c, n, s, [&] { return backward_pass(g, n, W, s, opt); });
+}
+
+// ---- messages kept in 8 bits ----------------------------------------------------------------------------------------------------
+static int check_saved8(const dr_heteroconv_saved8* S, const char* fn) {
+    DRC_REQUIRE(S != nullptr, "%s: null saved", fn);
+    for (const dr_act8* a : {&S->H_near, &S->H_pins, &S->H_pinned}) {
+        DRC_REQUIRE(a->q && a->scale, "%s: null checkpoint in saved", fn);
+        DRC_REQUIRE(aligned(a->q, 4) && aligned(a->scale, 8), "%s: misaligned checkpoint in saved", fn);
+    }
+    return DR_OK;
+}
+// What the passes below the checkpoints work with: the messages lie in the context's scratch, which a forward pass does not use otherwise (a
+// backward pass from checkpoints reads none).
+static dr_heteroconv_saved in_fp32(const dr_heteroconv* c, const dr_heteroconv_saved8* S) {
+    return dr_heteroconv_saved{S->vals_cell, S->idx_cell, S->vals_net, S->idx_net, c->dH, c->dH + (size_t)c->Nc * c->D, c->dH_pinned, S->mask,
+                               S->vals_cell_pins, S->idx_cell_pins, S->vals_net_self, S->idx_net_self};
+}
+
+extern "C" {
+
+int heteroconv_fwd_act8(dr_heteroconv* c, const float* X_cell, const float* X_net, const dr_heteroconv_weights* W, float* Y_cell,
+                        float* Y_net, const dr_heteroconv_saved8* S, void* stream) {
+    DRC_REQUIRE(c != nullptr, "heteroconv_fwd_act8: null context");
+    DRC_TRY(check_saved8(S, "heteroconv_fwd_act8"));
+    const hipStream_t s = as_stream(stream);
+    const dr_heteroconv_saved full = in_fp32(c, S);
+    const LayerFwd g{c, X_cell, X_net, Y_cell, Y_net, &full};
+    return in_scratch(&c, 1, s, [&]() -> int {
+        DRC_TRY(heteroconv_forward(&g, 1, W, s, ForwardOptions{}));
+        const Act8Pack jobs[3] = {{full.H_near, c->Nc, S->H_near}, {full.H_pinned, c->Nc, S->H_pinned}, {full.H_pins, c->Nn, S->H_pins}};
+        return launch_act8_packs(jobs, 3, c->D, s);
+    });
+}
+
+int heteroconv_bwd_act8(dr_heteroconv* c, const float* dY_cell, const float* dY_net, const dr_heteroconv_weights* W,
+                        const dr_heteroconv_saved8* S, float* dX_cell, float* dX_net, const dr_heteroconv_wgrads* dW, void* stream) {
+    DRC_REQUIRE(c != nullptr, "heteroconv_bwd_act8: null context");
+    DRC_TRY(check_saved8(S, "heteroconv_bwd_act8"));
+    DRC_REQUIRE(dW && dW->self_near && dW->neigh_near && dW->self_pins && dW->neigh_pins && dW->pinned,
+                "heteroconv_bwd_act8: null weight gradient");
+    const dr_heteroconv_saved full = in_fp32(c, S);
+    const LayerBwd g{c, dY_cell, dY_net, &full, dX_cell, dX_net, *dW};
+    BackwardOptions opt;
+    opt.saved8 = S;
+    return heteroconv_backward(&g, 1, W, as_stream(stream), opt);
+}
+
+}  // extern "C"
