@@ -191,7 +191,7 @@ int dr_act8_wgrad(const dr_act8* A, int64_t n, int32_t D, const float* dZ, int32
  *     N     = norm(X_out) * w_before + b_before                             (the next layer's input)
  *     norm(x) = x * r,  r = 1 / sqrt(mean(x^2) + eps)                 DR_ROWNORM_RMS
  *     norm(x) = (x - m) * r,  m = mean(x), r = 1 / sqrt(mean((x - m)^2) + eps)      DR_ROWNORM_LAYER
- * Means are over the D entries of a row.  G has gate_cols columns: D (a gate per element), 1 (one per row) or 0 (no gate,
+ * Means are over the D entries of a row, in fp32: a row whose squares overflow has r = 0.  G has gate_cols columns: D (a gate per element), 1 (one per row) or 0 (no gate,
  * G NULL).  w_*, b_* and scale are [D]; NULL stands for ones, zeros and ones.
  * Y NULL: only the norm in front, N of X (X_out, G, y and g are NULL then, and saved.x is the checkpoint of X).
  * N NULL: only the part behind the layer.  One of Y and N is given.
@@ -201,7 +201,7 @@ int dr_act8_wgrad(const dr_act8* A, int64_t n, int32_t D, const float* dZ, int32
 typedef struct dr_block {
     int32_t norm;                 /* DR_ROWNORM_*, of both norms */
     int32_t gate_cols;            /* 0, 1 or D */
-    float eps;                    /* > 0 */
+    float eps;                    /* > 0, a normal number */
     const float *w_after, *b_after, *scale, *w_before, *b_before;
 } dr_block;
 /* What the forward pass leaves for the backward pass; every part may be NULL in the forward pass and is not kept then.
@@ -211,7 +211,7 @@ typedef struct dr_block_saved {
     float *stats_after, *stats_before;
     dr_act8 x, y, g;
 } dr_block_saved;
-/* X_out and N may be X, Y or G themselves, at the same address: every row is read before it is written. */
+/* X_out and N may be X, Y or a G of D columns themselves, at the same address: every row is read before it is written. */
 int dr_block_fwd(const dr_block* block, int64_t n, int32_t D, const float* X, const float* Y, const float* G, float* X_out,
                  float* N, const dr_block_saved* saved, void* stream);
 
@@ -221,7 +221,8 @@ int dr_block_fwd(const dr_block* block, int64_t n, int32_t D, const float* X, co
  * front.  The statistics are the saved ones, so that with checkpoints the gradient is the formula's at the values that the
  * checkpoints stand for, with the statistics of the exact rows.
  * dX[n,D] (of the residual input; without Y, of the norm's input), dY[n,D], dG[n,gate_cols] and the sums over rows dw_after, db_after, dscale,
- * dw_before, db_before [D] are overwritten; NULL = not wanted.  dX and dY may be dX_out, dN or a given Y, X_out or G themselves.
+ * dw_before, db_before [D] are overwritten; NULL = not wanted.  dX, dY and a dG of D columns may be dX_out, dN or a given Y, X_out or G (of D
+ * columns) themselves, each another one; a dG of one column may be its G.
  * workspace: at least dr_block_bwd_workspace_bytes() bytes, 256-byte aligned, contents undefined before and after; it
  * belongs to one call at a time.  Sums over rows have a fixed order: a pass is reproducible bit for bit.
  */

@@ -213,7 +213,7 @@ int dr_act8_wgrad(const dr_act8* A, int64_t n, int32_t D, const float* dZ, int32
 static int check_block(const dr_block* b, int32_t D, const char* fn) {
     DRC_REQUIRE(b != nullptr, "%s: null block", fn);
     DRC_REQUIRE(b->norm == DR_ROWNORM_RMS || b->norm == DR_ROWNORM_LAYER, "%s: unknown norm %d", fn, b->norm);
-    DRC_REQUIRE(b->eps > 0.0f && b->eps < 1e30f, "%s: eps must be positive", fn);
+    DRC_REQUIRE(b->eps >= 1.17549435e-38f && b->eps < 1e30f, "%s: eps must be positive and a normal number", fn);
     DRC_REQUIRE(b->gate_cols == 0 || b->gate_cols == 1 || b->gate_cols == D, "%s: gate_cols = %d is not 0, 1 or D = %d", fn, b->gate_cols, D);
     DRC_REQUIRE(aligned(b->w_after, 4) && aligned(b->b_after, 4) && aligned(b->scale, 4) && aligned(b->w_before, 4) && aligned(b->b_before, 4),
                 "%s: misaligned parameter vector", fn);
@@ -274,7 +274,8 @@ int dr_block_bwd(const dr_block* block, int64_t n, int32_t D, const float* dX_ou
         if (S.y.q) DRC_TRY(check_act8(&S.y, "dr_block_bwd", "y"));
         if (S.g.q) DRC_TRY(check_act8(&S.g, "dr_block_bwd", "g"));
     }
-    DRC_REQUIRE(g.dX == nullptr || g.dX != g.dY, "dr_block_bwd: dX and dY are the same");
+    DRC_REQUIRE((g.dX == nullptr || (g.dX != g.dY && g.dX != g.dG)) && (g.dY == nullptr || g.dY != g.dG),
+                "dr_block_bwd: two of dX, dY and dG are the same");
     DRC_REQUIRE(aligned(dX_out, 4) && aligned(dN, 4) && aligned(X_out, 4) && aligned(Y, 4) && aligned(G, 4) && aligned(S.stats_after, 4) &&
                     aligned(S.stats_before, 4) && aligned(g.dX, 4) && aligned(g.dY, 4) && aligned(g.dG, 4) && aligned(g.dw_after, 4) &&
                     aligned(g.db_after, 4) && aligned(g.dscale, 4) && aligned(g.dw_before, 4) && aligned(g.db_before, 4),

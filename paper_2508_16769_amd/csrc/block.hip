@@ -177,7 +177,9 @@ template <typename T, int FROM> struct Incoming {
 // Columns past the width hold whatever the arithmetic makes of zeros: parameters are zeros there, so they add nothing to a row's sums, and
 // they are neither stored nor part of the sums over rows.  Rows past the end are zeros throughout, their statistics among them; so is all that
 // belongs to a part that is left out.
-template <typename T, int GATE, int FROM> __global__ __launch_bounds__(kRowThreads) void block_bwd_kernel(BlockBwd a) {
+// Rows of any width have 1024 workgroups: all of them resident, four wavefronts per SIMD.
+template <typename T, int GATE, int FROM>
+__global__ __launch_bounds__(kRowThreads, T::W == 1 && FROM != kEither ? 4 : 1) void block_bwd_kernel(BlockBwd a) {
     __shared__ float sh[2][kRowThreads / kWave][2];
     __shared__ float all[T::R][T::LPR * T::E];
     RowSums sums{sh, 0};

@@ -1043,12 +1043,17 @@ __device__ __forceinline__ void wgrad_side(const DRC_CONST SEG* seg, bf16x8* sme
     }
 }
 
+// entry e of a graph's sums: the cells' three products, then the nets' two
+template <int D> __device__ __forceinline__ void list_sums(const DRC_CONST WgradSeg* cells, const DRC_CONST WgradSeg* nets, int e, PartialSum* to) {
+    const int prod = e < 3 ? e : e - 3;
+    const DRC_CONST WgradSeg* const g = e < 3 ? cells : nets;
+    const int n = g->wgs * WTile<D>::KG;
+    *to = PartialSum{g->scratch + (size_t)prod * n * D * D, g->dW[prod], n, D * D};
+}
 template <int D, typename ARGS> __device__ __forceinline__ void wgrad_workgroup(const DRC_CONST ARGS* k, bf16x8* smem, int wg) {
     if (k->table && wg == 0 && (int)threadIdx.x < k->n / 2 * kSumsPerGraph) {      // cells and nets in turn
-        const int q = threadIdx.x / kSumsPerGraph, e = threadIdx.x % kSumsPerGraph, prod = e < 3 ? e : e - 3;
-        const DRC_CONST WgradSeg* const g = k->s + 2 * q + (e < 3 ? 0 : 1);
-        const int n = g->wgs * WTile<D>::KG;
-        k->table[threadIdx.x] = PartialSum{g->scratch + (size_t)prod * n * D * D, g->dW[prod], n, D * D};
+        const int q = threadIdx.x / kSumsPerGraph, e = threadIdx.x % kSumsPerGraph;
+        list_sums<D>(k->s + 2 * q, k->s + 2 * q + 1, e, k->table + threadIdx.x);
     }
     int q = 0;
     while (q + 1 < k->n && wg >= k->s[q + 1].wg0) ++q;
@@ -1060,18 +1065,6 @@ template <int D>
 __global__ __launch_bounds__(Tile<D>::THREADS, 2) void wgrad_partial_kernel(WgradArgs<kMaxGraphs> a) {
     extern __shared__ bf16x8 smem8[];
     wgrad_workgroup<D>(kernel_args<WgradArgs<kMaxGraphs>>(), smem8, blockIdx.x);
-}
-
-// One graph's weight gradients from messages kept in 8 bits: the cells' workgroups, then the nets'.
-struct Wgrad8Args { Wgrad8Seg s[2]; int n; };
-template <int D>
-__global__ __launch_bounds__(Tile<D>::THREADS, 2) void saved8_wgrad_kernel(Wgrad8Args a) {
-    extern __shared__ bf16x8 smem8[];
-    const DRC_CONST Wgrad8Args* const k = kernel_args<Wgrad8Args>();
-    const DRC_CONST Wgrad8Seg* const g = k->s + (k->n > 1 && (int)blockIdx.x >= k->s[1].s.wg0 ? 1 : 0);
-    const int wg = (int)blockIdx.x - g->s.wg0;
-    if (g->s.mask) wgrad_side<D, true, true>(g, smem8, wg);
-    else wgrad_side<D, false, true>(g, smem8, wg);
 }
 
 // Weight gradients and projections of a backward pass in one launch.  Neither waits for the other, and while either has fewer tiles
@@ -1092,6 +1085,31 @@ __global__ __launch_bounds__(Tile<D>::THREADS, 2) void dense_bwd_kernel(DenseBwd
     if (wg < 0) wgrad_workgroup<D>(&k->wgrad, smem8, blockIdx.x);
     else if (wg < k->proj.cell_wgs) proj_bwd_side<D, true>(&k->proj, smem8, wg, k->proj.cell_wgs);
     else proj_bwd_side<D, false>(&k->proj, smem8, wg - k->proj.cell_wgs, k->proj.net_wgs);
+}
+
+// One graph's weight gradients from messages kept in 8 bits, the cells' workgroups, then the nets', and the projections beside them.
+struct Saved8BwdArgs {
+    ProjBwdArgs<1> proj;
+    Wgrad8Seg s[2];
+    PartialSum* table;            // null: wgrad_reduce_kernel follows, and there are no projections
+    int n, wgrad_wgs;
+};
+template <int D>
+__global__ __launch_bounds__(Tile<D>::THREADS, 2) void saved8_bwd_kernel(Saved8BwdArgs a) {
+    extern __shared__ bf16x8 smem8[];
+    const DRC_CONST Saved8BwdArgs* const k = kernel_args<Saved8BwdArgs>();
+    const int wg = (int)blockIdx.x - k->wgrad_wgs;
+    if (wg < 0) {
+        if (k->table && blockIdx.x == 0 && (int)threadIdx.x < kSumsPerGraph) list_sums<D>(&k->s[0].s, &k->s[1].s, threadIdx.x, k->table + threadIdx.x);
+        const DRC_CONST Wgrad8Seg* const g = k->s + (k->n > 1 && (int)blockIdx.x >= k->s[1].s.wg0 ? 1 : 0);
+        const int mine = (int)blockIdx.x - g->s.wg0;
+        if (g->s.mask) wgrad_side<D, true, true>(g, smem8, mine);
+        else wgrad_side<D, false, true>(g, smem8, mine);
+    } else if (wg < k->proj.cell_wgs) {
+        proj_bwd_side<D, true>(&k->proj, smem8, wg, k->proj.cell_wgs);
+    } else {
+        proj_bwd_side<D, false>(&k->proj, smem8, wg - k->proj.cell_wgs, k->proj.net_wgs);
+    }
 }
 
 // dW[i] = sum over a side's partials in a fixed order: wavefront w of the workgroup sums partials w, w + 16, ... of 64 x 4
@@ -1322,21 +1340,30 @@ static int launch_wgrads_to(const WgradJob* jobs, int n, int D, PartialSum* tabl
 }
 int launch_wgrads(const WgradJob* jobs, int n, int D, hipStream_t s) { return launch_wgrads_to(jobs, n, D, nullptr, s); }
 
-template <int D> static int launch_wgrads8_d(WgradArgs<kMaxGraphs>& a, const Wgrad8Job* jobs, hipStream_t s) {
+template <int D> static int launch_saved8_d(const WgradJob* plain, const Wgrad8Job* jobs, int n, const ProjBwdJob* proj,
+                                            const dr_heteroconv_weights* W, PartialSum* table, hipStream_t s) {
     using T = Tile<D>;
     static PerDevice cache;
+    constexpr size_t lds = dproj_lds<D>() > wgrad_lds<D>() ? dproj_lds<D>() : wgrad_lds<D>();
     int res = 0;
-    DRC_TRY(resident(&saved8_wgrad_kernel<D>, T::THREADS, wgrad_lds<D>(), cache, &res));
-    const int wgs = plan_wgrad<D>(a, res);
-    Wgrad8Args b{};
-    b.n = a.n;
-    for (int i = 0; i < a.n; ++i) b.s[i] = Wgrad8Seg{a.s[i], jobs[i].H1.scale, jobs[i].H2.scale};
-    hipLaunchKernelGGL((saved8_wgrad_kernel<D>), dim3((unsigned)wgs), dim3(T::THREADS), wgrad_lds<D>(), s, b);
-    hipLaunchKernelGGL((wgrad_reduce_kernel<D>), dim3((unsigned)(a.n * 3 * (D * D / 256))), dim3(64 * kRedWaves), 0, s, a);
+    DRC_TRY(resident(&saved8_bwd_kernel<D>, T::THREADS, lds, cache, &res));
+    WgradArgs<kMaxGraphs> a{};
+    set_wgrad(a, plain, n);
+    Saved8BwdArgs b{};
+    b.n = n;
+    b.table = table;
+    b.wgrad_wgs = plan_wgrad<D>(a, res);
+    for (int i = 0; i < n; ++i) b.s[i] = Wgrad8Seg{a.s[i], jobs[i].H1.scale, jobs[i].H2.scale};
+    if (proj) {
+        set_proj_bwd(b.proj, proj, 1, *W);
+        plan_proj_bwd<D>(b.proj, res);
+    }
+    hipLaunchKernelGGL((saved8_bwd_kernel<D>), dim3((unsigned)(b.wgrad_wgs + b.proj.cell_wgs + b.proj.net_wgs)), dim3(T::THREADS), lds, s, b);
+    if (!table) hipLaunchKernelGGL((wgrad_reduce_kernel<D>), dim3((unsigned)(n * 3 * (D * D / 256))), dim3(64 * kRedWaves), 0, s, a);
     DRC_HIP(hipGetLastError());
     return DR_OK;
 }
-int launch_wgrads8(const Wgrad8Job* jobs, int n, int D, hipStream_t s) {
+static int launch_saved8(const Wgrad8Job* jobs, int n, const ProjBwdJob* proj, const dr_heteroconv_weights* W, int D, PartialSum* table, hipStream_t s) {
     if (n < 1 || n > 2) return fail(DR_ERR_INVALID_ARG, "weight gradients of %d operands from checkpoints", n);
     WgradJob plain[2];
     for (int i = 0; i < n; ++i) {
@@ -1344,15 +1371,19 @@ int launch_wgrads8(const Wgrad8Job* jobs, int n, int D, hipStream_t s) {
         plain[i].H1 = reinterpret_cast<const float*>(jobs[i].H1.q);
         plain[i].H2 = reinterpret_cast<const float*>(jobs[i].H2.q);
     }
-    WgradArgs<kMaxGraphs> a{};
-    set_wgrad(a, plain, n);
     switch (D) {
-        case 32: return launch_wgrads8_d<32>(a, jobs, s);
-        case 64: return launch_wgrads8_d<64>(a, jobs, s);
-        case 96: return launch_wgrads8_d<96>(a, jobs, s);
-        case 128: return launch_wgrads8_d<128>(a, jobs, s);
+        case 32: return launch_saved8_d<32>(plain, jobs, n, proj, W, table, s);
+        case 64: return launch_saved8_d<64>(plain, jobs, n, proj, W, table, s);
+        case 96: return launch_saved8_d<96>(plain, jobs, n, proj, W, table, s);
+        case 128: return launch_saved8_d<128>(plain, jobs, n, proj, W, table, s);
         default: return fail(DR_ERR_UNSUPPORTED, "projection width D = %d not in {32,64,96,128}", D);
     }
+}
+int launch_wgrads8(const Wgrad8Job* jobs, int n, int D, hipStream_t s) { return launch_saved8(jobs, n, nullptr, nullptr, D, nullptr, s); }
+int launch_dense_bwd8(const Wgrad8Job* jobs, const ProjBwdJob* proj, const dr_heteroconv_weights& W, int D, PartialSum* table, PendingSums* pending,
+                      hipStream_t s) {
+    *pending = PendingSums{table, kSumsPerGraph, D * D};
+    return launch_saved8(jobs, 2, proj, &W, D, table, s);
 }
 
 template <int D> static int launch_dense_bwd_d(const WgradJob* wgrads, const ProjBwdJob* proj, int n, const dr_heteroconv_weights& W,

@@ -259,6 +259,9 @@ int launch_wgrads8(const Wgrad8Job* jobs, int n, int D, hipStream_t s);    // n 
 constexpr int kSumsPerGraph = 5;
 int launch_dense_bwd(const WgradJob* wgrads, const ProjBwdJob* proj, int n, const dr_heteroconv_weights& W, int D, PartialSum* table,
                      PendingSums* pending, hipStream_t s);
+// the same of one graph, cells and nets, from checkpoints
+int launch_dense_bwd8(const Wgrad8Job* jobs, const ProjBwdJob* proj, const dr_heteroconv_weights& W, int D, PartialSum* table, PendingSums* pending,
+                      hipStream_t s);
 int launch_pending_sums(const PendingSums& pending, hipStream_t s);
 
 // 8-bit activation checkpoints and residual blocks -----------------------------------------------------

@@ -657,12 +657,8 @@ static int backward_pass(const LayerBwd* g, int n, const dr_heteroconv_weights* 
     if (!alone) {
         if (!need_dx) return launch_wgrads(wj, 2 * n, D, s);
         PendingSums sums{};
-        if (opt.saved8) {
-            DRC_TRY(launch_wgrads8(w8, 2, D, s));
-            DRC_TRY(launch_proj_bwd(pj, n, *W, D, s));
-        } else {
-            DRC_TRY(launch_dense_bwd(wj, pj, n, *W, D, g[0].c->wg_sums, &sums, s));
-        }
+        if (opt.saved8) DRC_TRY(launch_dense_bwd8(w8, pj, *W, D, g[0].c->wg_sums, &sums, s));
+        else DRC_TRY(launch_dense_bwd(wj, pj, n, *W, D, g[0].c->wg_sums, &sums, s));
         for (int i = 0; i < n; ++i)
             if (g[i].c->near_plan)
                 DRC_TRY(launch_spmm_bwd_planned(g[i].c->near_plan, g[i].c->dH, cbsr_sets(g[i].c, g[i].S).i_near, g[i].c->k_near, g[i].c->S_cell, 1, s));

@@ -127,6 +127,18 @@ def test_widths(D):
         _check_backward(a, norm, dX_out, dN, o, ck, g)
 
 
+@pytest.mark.parametrize("D", [20, 64, 99, 300, 1000])
+def test_some_from_tensors_some_from_checkpoints(D):
+    rng = np.random.default_rng(D + 1)
+    n, norm = 90, "layer"
+    a = _inputs(rng, n, D, "full")
+    o, ck = _forward(a, norm, 1e-5, 8)
+    dX_out, dN = (0.1 * rng.standard_normal((2, n, D))).astype(np.float32)
+    for names in (("x8",), ("y8",), ("g8",), ("x8", "y8"), ("x8", "g8"), ("y8", "g8")):
+        some = {k: ck[k] for k in names}
+        _check_backward(a, norm, dX_out, dN, o, some, _backward(a, norm, dX_out, dN, o, some))
+
+
 @pytest.mark.parametrize("norm", list(NORMS))
 @pytest.mark.parametrize("D", [64, 77])
 def test_parts_left_out(norm, D):

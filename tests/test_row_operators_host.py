@@ -72,7 +72,7 @@ def test_block_forward_refusals():
         b = block() if b is None else b
         s = saved() if s is None else s
         return lib.dr_block_fwd(None if null else ref(b), n, D, X, Y, G, Xo, N, ref(s), None)
-    bad = (dict(null=True), dict(b=block(norm=2)), dict(b=block(eps=0.0)), dict(b=block(eps=-1.0)), dict(b=block(eps=float("nan"))),
+    bad = (dict(null=True), dict(b=block(norm=2)), dict(b=block(eps=0.0)), dict(b=block(eps=-1.0)), dict(b=block(eps=1e-40)), dict(b=block(eps=float("inf"))), dict(b=block(eps=float("nan"))),
            dict(b=block(gate=3), G=A), dict(b=block(gate=8)), dict(b=block(gate=0), G=A), dict(b=block(w=ODD)), dict(n=-1), dict(n=1 << 31),
            dict(D=0), dict(X=None), dict(X=ODD), dict(Y=ODD), dict(N=ODD), dict(Xo=None), dict(Y=None), dict(Y=None, Xo=None, N=None),
            dict(Xo=A + 32), dict(N=None), dict(Y=None, Xo=None), dict(Y=None, Xo=None, s=saved(sa=None, y=ck())),
@@ -97,7 +97,8 @@ def test_block_backward_refusals():
     bad = (dict(null=True), dict(no_grads=True), dict(n=-1), dict(D=0), dict(dXo=None, dN=None), dict(Xo=None), dict(s=saved(x=ck())),
            dict(s=saved(y=ck())), dict(b=block(gate=8), G=A, s=saved(g=ck())), dict(s=saved(sa=None)), dict(s=saved(sb=None)),
            dict(b=block(gate=1)), dict(G=A), dict(b=block(gate=1), s=saved(g=ck())), dict(Y=None), dict(Y=None, G=A, b=block(gate=1), g=only_front),
-           dict(g=dr_block_grads(A, A, None, A, A, A, A, A)), dict(g=dr_block_grads(A, A + 16, A, A, A, A, A, A)), dict(dXo=ODD),
+           dict(g=dr_block_grads(A, A, None, A, A, A, A, A)), dict(b=block(gate=8), G=A, g=dr_block_grads(A, A + 16, A, A, A, A, A, A)),
+           dict(b=block(gate=8), G=A, g=dr_block_grads(A, A + 16, A + 16, A, A, A, A, A)), dict(g=dr_block_grads(A, A + 16, A, A, A, A, A, A)), dict(dXo=ODD),
            dict(g=dr_block_grads(A, A + 16, None, ODD, A, A, A, A)), dict(ws=None), dict(ws=A + 16))
     for kw in bad:
         assert call(**kw) == P.DR_ERR_INVALID_ARG, kw
