@@ -177,9 +177,7 @@ template <typename T, int FROM> struct Incoming {
 // Columns past the width hold whatever the arithmetic makes of zeros: parameters are zeros there, so they add nothing to a row's sums, and
 // they are neither stored nor part of the sums over rows.  Rows past the end are zeros throughout, their statistics among them; so is all that
 // belongs to a part that is left out.
-// Rows of any width have 1024 workgroups: all of them resident, four wavefronts per SIMD.
-template <typename T, int GATE, int FROM>
-__global__ __launch_bounds__(kRowThreads, T::W == 1 && FROM != kEither ? 4 : 1) void block_bwd_kernel(BlockBwd a) {
+template <typename T, int GATE, int FROM> __global__ __launch_bounds__(kRowThreads) void block_bwd_kernel(BlockBwd a) {
     __shared__ float sh[2][kRowThreads / kWave][2];
     __shared__ float all[T::R][T::LPR * T::E];
     RowSums sums{sh, 0};
@@ -380,17 +378,17 @@ int launch_block_bwd(BlockBwd a, void* ws, hipStream_t s) {
         DRC_TRY(with_row_tile(a.D, vector, [&](auto tile) -> int {
             using T = decltype(tile);
             const int64_t blocks = (a.n + T::R - 1) / T::R;
-            a.parts = (int)(blocks < kBlockWgs<T> ? blocks : kBlockWgs<T>);
+            auto start = [&](auto gate, auto from) {
+                constexpr int GATE = decltype(gate)::value, FROM = decltype(from)::value;
+                // (where the registers of four elements, their gates and codes leave a SIMD three wavefronts: as many as are resident)
+                constexpr int64_t most = T::W == 1 && T::E == 4 && (FROM == kEither || (FROM == kCodes && GATE == kFullGate)) ? 768 : kBlockWgs<T>;
+                a.parts = (int)(blocks < most ? blocks : most);
+                hipLaunchKernelGGL((block_bwd_kernel<T, GATE, FROM>), dim3((unsigned)a.parts), dim3(kRowThreads), 0, s, a);
+            };
             auto go = [&](auto gate) {
-                constexpr int GATE = decltype(gate)::value;
-                const dim3 grid((unsigned)a.parts);
-                if (!codes) {
-                    hipLaunchKernelGGL((block_bwd_kernel<T, GATE, kFloats>), grid, dim3(kRowThreads), 0, s, a);
-                } else if (!floats) {
-                    hipLaunchKernelGGL((block_bwd_kernel<T, GATE, kCodes>), grid, dim3(kRowThreads), 0, s, a);
-                } else if constexpr (T::W == 1) {
-                    hipLaunchKernelGGL((block_bwd_kernel<T, GATE, kEither>), grid, dim3(kRowThreads), 0, s, a);
-                }
+                if (!codes) start(gate, std::integral_constant<int, kFloats>{});
+                else if (!floats) start(gate, std::integral_constant<int, kCodes>{});
+                else if constexpr (T::W == 1) start(gate, std::integral_constant<int, kEither>{});
             };
             by_gate(a.b.gate_cols, a.D, go);
             DRC_HIP(hipGetLastError());
