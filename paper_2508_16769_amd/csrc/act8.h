@@ -46,7 +46,7 @@ template <int W_, int LPR_, int V_> struct RowTile {
     static constexpr int E = V * W;                             // elements per lane
     static constexpr int R = kRowThreads / LPR;                 // rows per workgroup
     static constexpr int GL = 32 / W < LPR ? 32 / W : LPR;      // lanes of a group
-    static_assert(E <= 4 && LPR <= kRowThreads && R <= 64);
+    static_assert(E <= 4 && LPR <= kRowThreads && R <= 64 && (V == 1 || W * LPR % 32 == 0));
 };
 // this lane's places in the rows of a workgroup
 template <typename T> struct RowLane {
@@ -224,10 +224,14 @@ template <typename F> int with_row_tile(int D, bool vector, F f) {
     if (D <= 8) return f(RowTile<1, 8, 1>{});
     if (D <= 16) return f(RowTile<1, 16, 1>{});
     if (D <= 32) return f(RowTile<1, 32, 1>{});
-    if (D <= 64) return f(RowTile<1, 64, 1>{});
-    if (D <= 128) return f(RowTile<1, 64, 2>{});
+    if (D <= 64) return f(RowTile<1, 32, 2>{});
+    if (D <= 96) return f(RowTile<1, 32, 3>{});
+    if (D <= 128) return f(RowTile<1, 32, 4>{});
+    if (D <= 192) return f(RowTile<1, 64, 3>{});
     if (D <= 256) return f(RowTile<1, 64, 4>{});
+    if (D <= 384) return f(RowTile<1, 128, 3>{});
     if (D <= 512) return f(RowTile<1, 128, 4>{});
+    if (D <= 768) return f(RowTile<1, 256, 3>{});
     return f(RowTile<1, 256, 4>{});
 }
 

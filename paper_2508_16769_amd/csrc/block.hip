@@ -322,9 +322,13 @@ __global__ __launch_bounds__(kWave* kSumWaves) void block_sums_kernel(const floa
 
 // Workgroups of a launch: few that walk many rows.  Two per compute unit draw 5.6 TB/s from memory, more of them drift apart and find its
 // pages closed: 1.2 M x 128, 512 / 768 / 1024 / 2048 workgroups, us: forward 443 / 486 / 530 / 580, backward from checkpoints 496 / 552 / 590 /
-// 610; 60 000 x 128 24.4 / 25.4 / 25.7 / 26.0 and 32.8 / 34.5 / 35.5 / 39.4; 256 leave a SIMD one wavefront (528 and 605).  Rows of any width have a
-// quarter as much in flight per lane: 200 000 x 77, 512 / 1024 / 2048: 95 / 61 / 69 and 119 / 91 / 98.
-template <typename T> constexpr int kBlockWgs = T::W == 4 ? 512 : 1024;
+// 610; 60 000 x 128 24.4 / 25.4 / 25.7 / 26.0 and 32.8 / 34.5 / 35.5 / 39.4; 256 leave a SIMD one wavefront (528 and 605).  Rows of any width are
+// read a column at a time, and take three: 200 000 x 77, 512 / 768 / 1024: forward 58 / 55 / 58, with checkpoints 89 / 83 / 85, backward from
+// checkpoints 81 / 73 / 78; 500 000 x 45 123 / 94 / 88, 151 / 140 / 138, 157 / 129 / 125; 20 000 x 999 61 / 64 / 66, 86 / 83 / 84, 86 / 84 / 87.
+template <typename T> constexpr int kBlockWgs = T::W == 4 ? 512 : 768;
+// Forward with a gate per element and checkpoints, ten tensors at once: one per compute unit, 256 / 512 workgroups, 500 000 x 128 290 / 314,
+// 1 M x 64 287 / 313; not where the caches hold them (60 000 x 128 41 / 37).
+constexpr int64_t kManyTensorsFrom = int64_t(1) << 25;     // elements
 static bool vector_rows(int D, std::initializer_list<const void*> f32, std::initializer_list<const void*> q) {
     bool v = D % 4 == 0;
     for (const void* p : f32) v = v && aligned(p, 16);
@@ -344,7 +348,9 @@ int launch_block_fwd(const BlockFwd& a, hipStream_t s) {
     return with_row_tile(a.D, vector, [&](auto tile) -> int {
         using T = decltype(tile);
         const int64_t rows = ckpt ? (a.n + 7) / 8 * 8 : a.n, blocks = (rows + T::R - 1) / T::R;
-        const dim3 grid((unsigned)(blocks < kBlockWgs<T> ? blocks : kBlockWgs<T>));
+        const bool many = T::W == 4 && ckpt && a.b.gate_cols == a.D && a.n * a.D >= kManyTensorsFrom;
+        const int64_t most = many ? kBlockWgs<T> / 2 : kBlockWgs<T>;
+        const dim3 grid((unsigned)(blocks < most ? blocks : most));
         auto go = [&](auto gate) {
             constexpr int GATE = decltype(gate)::value;
             if (ckpt) hipLaunchKernelGGL((block_fwd_kernel<T, GATE, true>), grid, dim3(kRowThreads), 0, s, a);
@@ -378,12 +384,9 @@ int launch_block_bwd(BlockBwd a, void* ws, hipStream_t s) {
         DRC_TRY(with_row_tile(a.D, vector, [&](auto tile) -> int {
             using T = decltype(tile);
             const int64_t blocks = (a.n + T::R - 1) / T::R;
+            a.parts = (int)(blocks < kBlockWgs<T> ? blocks : kBlockWgs<T>);
             auto start = [&](auto gate, auto from) {
-                constexpr int GATE = decltype(gate)::value, FROM = decltype(from)::value;
-                // (where the registers of four elements, their gates and codes leave a SIMD three wavefronts: as many as are resident)
-                constexpr int64_t most = T::W == 1 && T::E == 4 && (FROM == kEither || (FROM == kCodes && GATE == kFullGate)) ? 768 : kBlockWgs<T>;
-                a.parts = (int)(blocks < most ? blocks : most);
-                hipLaunchKernelGGL((block_bwd_kernel<T, GATE, FROM>), dim3((unsigned)a.parts), dim3(kRowThreads), 0, s, a);
+                hipLaunchKernelGGL((block_bwd_kernel<T, decltype(gate)::value, decltype(from)::value>), dim3((unsigned)a.parts), dim3(kRowThreads), 0, s, a);
             };
             auto go = [&](auto gate) {
                 if (!codes) start(gate, std::integral_constant<int, kFloats>{});
