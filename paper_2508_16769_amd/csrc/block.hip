@@ -57,7 +57,8 @@ __device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf
 // Statistics are [n] (r) or [n,2] (m, r).  A mean that is not there is read from outside, as zero.
 struct StatsLane {
     int m, r;
-    __device__ __forceinline__ StatsLane(int row, bool layer, bool on) : m(on && layer ? row * 8 : kOutside), r(on ? (layer ? row * 8 + 4 : row * 4) : kOutside) {}
+    __device__ __forceinline__ StatsLane(int row, bool layer, bool on)
+        : m(on && layer ? row * 8 : kOutside), r(on ? (layer ? row * 8 + 4 : row * 4) : kOutside) {}
 };
 __device__ __forceinline__ Buf stats_view(const float* p, int64_t r0, int left, bool layer) { return rows_view(p, r0, left, layer ? 8 : 4); }
 
@@ -374,12 +375,15 @@ int launch_block_bwd(BlockBwd a, void* ws, hipStream_t s) {
     if (!a.dN) {                  // nothing of the norm in front is read, so that nothing in it counts
         a.X_out = nullptr;
         a.saved.x = dr_act8{};
+        a.saved.stats_before = nullptr;
     }
     const bool full = a.b.gate_cols == a.D;
     const bool floats = a.X_out || a.Y || (full && a.G), codes = a.saved.x.q || a.saved.y.q || a.saved.g.q;
     // (some from tensors, some from checkpoints: the kernels of any width)
-    const bool vector = !(floats && codes) && vector_rows(a.D, {a.dX_out, a.dN, a.X_out, a.Y, full ? a.G : nullptr, a.grads.dX, a.grads.dY, full ? a.grads.dG : nullptr},
-                                    {a.saved.x.q, a.saved.y.q, a.saved.g.q});
+    const bool vector = !(floats && codes) && vector_rows(a.D,
+                                                          {a.dX_out, a.dN, a.X_out, a.Y, full ? a.G : nullptr, a.grads.dX, a.grads.dY,
+                                                           full ? a.grads.dG : nullptr},
+                                                          {a.saved.x.q, a.saved.y.q, a.saved.g.q});
     a.part = static_cast<float*>(ws);
     a.parts = 0;
     if (a.n > 0)

@@ -221,6 +221,25 @@ def test_wild_rows_stay_by_themselves():
     assert not g["dG"][120:122].any()
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_nothing_of_a_norm_that_is_left_out_counts(bits):
+    """Without dN the rows and statistics of the norm in front are not part of the gradient, whatever they hold."""
+    rng = np.random.default_rng(10)
+    n, D, norm = 50, 64, "layer"
+    a = _inputs(rng, n, D, "none")
+    o, ck = _forward(a, norm, 1e-5, bits)
+    dX_out = (0.1 * rng.standard_normal((n, D))).astype(np.float32)
+    want = _backward(a, norm, dX_out, None, o, ck)
+    o["X_out"].fill_(float("inf"))
+    o["stats_before"].fill_(float("nan"))
+    if bits == 8:
+        ck["x8"][1].fill_(255)
+    got = _backward(a, norm, dX_out, None, o, ck)
+    for k in ("dX", "dY", "dw_after", "db_after", "dscale", "dw_before", "db_before"):
+        assert torch.equal(got[k], want[k]), k
+    assert torch.equal(got["dX"], dev(dX_out)) and not got["dw_before"].any()
+
+
 def test_rows_at_any_alignment():
     rng = np.random.default_rng(11)
     n, D, norm = 60, 64, "layer"
