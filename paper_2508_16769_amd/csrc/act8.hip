@@ -1,6 +1,7 @@
 // 8-bit activation checkpoints: packing, unpacking, and weight gradients of projections whose input is held as one.
 #include "act8.h"
 
+#include <cmath>
 #include <type_traits>
 
 namespace drc {
@@ -133,11 +134,12 @@ template <int TD_, int TF_, int WA_, int WB_> struct GradTile {
     static constexpr int CR = 32 * WK, RG = CR / 8;             // rows and units per column of a chunk
     static constexpr int AU = RG * TD, BU = RG * TF;            // units of A and of one part of dZ
     static constexpr int BUF = AU + 3 * BU;
-    static constexpr int M = TD / WA >= 32 && TF / WB >= 32 ? 32 : 16;  // width of a block
+    static constexpr int M = TD / WA % 32 == 0 && TF / WB % 32 == 0 ? 32 : 16;     // width of a block
     static constexpr int MA = TD / (M * WA), MB = TF / (M * WB);        // blocks per wavefront
     static constexpr int KS = M / 16;                                   // matrix instructions per block, part and chunk
     typedef float Block __attribute__((ext_vector_type(M * M / 64)));
-    static_assert(AU <= kGradThreads && BU <= kGradThreads && AU % 64 == 0 && BU % 64 == 0 && MA >= 1 && MB >= 1);
+    static_assert(AU <= kGradThreads && BU <= kGradThreads && AU % 64 == 0 && BU % 64 == 0);
+    static_assert(MA * M * WA == TD && MB * M * WB == TF && TD * TF % 256 == 0);
 };
 
 struct GradArgs {
@@ -383,7 +385,8 @@ __global__ __launch_bounds__(64 * kSumWaves) void act8_wgrad_sum_kernel(const fl
         }
 }
 
-// Calls f(GradTile<...>{}): a tile as wide as the matrix, up to 128 either way.
+// Calls f(GradTile<...>{}): a tile as wide as the matrix, up to 128 either way.  Tiles of 96 columns for the layers' width: 250 000 x 96 x 96 41.5 / 38.5 us,
+// 60 013 x 96 x 200 26.5 / 24.5 (128 x 128 / 96).
 template <typename F> static int with_grad_tile(int D, int Fw, F f) {
     if (D <= 32) {
         if (Fw <= 32) return f(GradTile<32, 32, 2, 1>{});
@@ -395,15 +398,24 @@ template <typename F> static int with_grad_tile(int D, int Fw, F f) {
         if (Fw <= 64) return f(GradTile<64, 64, 2, 2>{});
         return f(GradTile<64, 128, 2, 4>{});
     }
+    if (D <= 96 && Fw > 64) return f(GradTile<96, 128, 2, 4>{});
+    if (Fw > 64 && Fw <= 96) return f(GradTile<128, 96, 4, 2>{});
     if (Fw <= 32) return f(GradTile<128, 32, 4, 2>{});
     if (Fw <= 64) return f(GradTile<128, 64, 4, 2>{});
     return f(GradTile<128, 128, 2, 4>{});
 }
-// Workgroups per tile of dW: one per compute unit in all, a chunk each at least.
+// Workgroups per tile of dW.  A workgroup's partial sums weigh as much as a few chunks, written once and read once: with r chunks a workgroup a launch
+// takes about r * c + tiles * chunks / r * s, least at r = sqrt(tiles * chunks * s / c).  s / c is near 0.045 whatever the tile (best r measured: 32 x 32
+// 157 / 469 / 1 953 chunks 4 / 5 / 10; 64 x 64 157 / 313 / 938 2.5 / 4 / 6.5; 128 x 128 128 / 250 / 500 2 / 3.5 / 4.5).  No more than one per compute
+// unit in all, and all with the same number of chunks but for the last.  One per compute unit, or a chunk each / now: 10 000 x 64 x 64 13.0 / 10.6 us,
+// 20 000 16.7 / 12.4, 8 000 x 128 x 128 17.7 / 13.6, 60 000 x 32 x 32 20.0 / 14.3.
 template <typename T> static int grad_splits(int64_t n, int D, int F) {
     const int64_t tiles = (int64_t)((D + T::TD - 1) / T::TD) * ((F + T::TF - 1) / T::TF), chunks = (n + T::CR - 1) / T::CR;
     const int64_t most = tiles < kGradWgs ? kGradWgs / tiles : 1;
-    return (int)(chunks < 1 ? 1 : chunks < most ? chunks : most);
+    int64_t r = (int64_t)(std::sqrt(0.045 * (double)(tiles * chunks)) + 0.5);
+    if (r * most < chunks) r = (chunks + most - 1) / most;
+    if (r < 1) r = 1;
+    return chunks < 1 ? 1 : (int)((chunks + r - 1) / r);
 }
 
 size_t act8_wgrad_workspace(int64_t n, int D, int F) {
