@@ -113,11 +113,11 @@ int launch_act8_unpack(const dr_act8& in, int64_t n, int D, float* X, hipStream_
 // multiply, the other half after, so that vector and matrix instructions of a SIMD's two wavefronts overlap.  A workgroup takes one tile of
 // dW and every S-th chunk; partial sums go to the workspace and are added by a second kernel, in 64 bits and a fixed order.
 //
-// What bounds it is issue: 1.2 M x 128 x 128 takes 171 us with the sums (773 MB, 4.5 TB/s); without the multiplication 127 (memory), with the
+// What bounds it is issue: 1.2 M x 128 x 128 takes 171 to 184 us by card, with the sums (773 MB, 4.5 to 4.2 TB/s); without the multiplication 127 (memory), with the
 // multiplication and bare staging 138.  Vector and matrix instructions of a SIMD take turns for the most part, 99 of the former per wavefront and
 // chunk (130 before: codes sign-extended as they are loaded, scale bytes shifted into place by one instruction, rows past the end looked for once per
-// chunk, running sums added to every 16 chunks; 191 us).  60 013 x 96 x 200, 24 us: 15 chunks a workgroup one after the other, tiles of 128 columns
-// for 96 and 72; 2 048 x 64 x 64, 9 us of two launches.
+// chunk, running sums added to every 16 chunks; 191 us).  60 013 x 96 x 200, 23 us: 15 chunks a workgroup one after the other, tiles of 128 columns
+// for 72; 2 048 x 64 x 64, 8.3 us of two launches.
 // ---------------------------------------------------------------------------------------------------
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
