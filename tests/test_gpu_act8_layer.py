@@ -96,6 +96,20 @@ def test_schedules_and_kernel_times(mode):
     layer.heteroconv_destroy()
 
 
+def test_placed_cells_on_staged_tiles():
+    """`near` in the order of a placement: its transposed DR-SpMM runs on staged tiles, beside nothing of the checkpoints."""
+    rng = np.random.default_rng(9)
+    Nc, Nn, D = 50_000, 3_000, 64
+    near = ((np.arange(Nc)[:, None] + np.array([-4, -3, -2, -1, 1, 2, 3, 4])) % Nc).astype(np.int32).ravel()
+    rel = [P.Csr(Nc, Nc, dev(8 * np.arange(Nc + 1, dtype=np.int32)), dev(near), dev(np.full(8 * Nc, 0.125, np.float32)))]
+    rel += [P.Csr(m, n, *(dev(a) for a in random_csr(rng, m, n, 3, dup=True))) for m, n in ((Nn, Nc), (Nc, Nn))]
+    layer = P.HeteroConv(*rel, D, 16, 16)
+    assert layer.heteroconv_set_cell_order(dev(np.arange(Nc, dtype=np.int32)))
+    t = _tensors(rng, Nc, Nn, D)
+    _check(_run(layer, t, False), _run(layer, t, True), t, layer)
+    layer.heteroconv_destroy()
+
+
 def test_passes_on_alternating_streams():
     """The messages of a forward pass lie in the context's scratch: passes on several streams follow one another by themselves."""
     rng = np.random.default_rng(6)
