@@ -121,7 +121,8 @@ def block_bwd(dX_out=None, dN=None, X_out=None, stats_before=None, Y=None, stats
         sig = np.ones((n, 1)) if G is None else _sigmoid(G)
         du, adu = d * sc * sig, ad * np.abs(sc) * sig
         if G is not None:
-            dG, adG = d * sc * u * sig * (1 - sig), ad * np.abs(sc) * au * sig
+            shut = _sigmoid(-G)                       # 1 - sig
+            dG, adG = d * sc * u * sig * shut, ad * np.abs(sc) * au * sig * shut
             if G.shape[1] == 1 and D > 1:
                 dG, adG = dG.sum(1, keepdims=True), adG.sum(1, keepdims=True)
             out["dG"], mag["dG"] = dG, adG

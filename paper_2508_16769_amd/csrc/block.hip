@@ -52,7 +52,15 @@ __device__ __forceinline__ void row_stats(const float (&x)[T::E], const RowLane<
     }
     r = __builtin_amdgcn_rsqf(fmaf(sums.sum<T>(s), inv, eps));       // (off by an ulp at most)
 }
-__device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.0f + expf(-g)); }
+// sigmoid(g) and 1 - sigmoid(g).  (The reciprocal is off by an ulp at most; a gate below -87, whose sigmoid is a denormal, is shut.)  An open gate's
+// complement is e^-g * sigmoid(g): as a difference from 1 nothing of it is left from g = 17 on, where it is 4e-8.
+struct Sigmoid {
+    float open, shut;
+};
+__device__ __forceinline__ Sigmoid sigmoid(float g) {
+    const float e = expf(-g), open = __builtin_amdgcn_rcpf(1.0f + e);
+    return {open, g > 0.f ? e * open : 1.0f - open};
+}
 
 // Statistics are [n] (r) or [n,2] (m, r).  A mean that is not there is read from outside, as zero.
 struct StatsLane {
@@ -103,7 +111,7 @@ template <typename T, int GATE, bool CKPT> __global__ __launch_bounds__(kRowThre
         take(ry, y);
         if constexpr (GATE == kFullGate) take(rg, g);
         if constexpr (GATE == kRowGate) {
-            const float one = sigmoid(of_bits(r1));
+            const float one = sigmoid(of_bits(r1)).open;
 #pragma unroll
             for (int i = 0; i < T::E; ++i) g[i] = one;
         }
@@ -119,7 +127,7 @@ template <typename T, int GATE, bool CKPT> __global__ __launch_bounds__(kRowThre
         }
         if constexpr (GATE == kFullGate) {
 #pragma unroll
-            for (int i = 0; i < T::E; ++i) g[i] = sigmoid(g[i]);
+            for (int i = 0; i < T::E; ++i) g[i] = sigmoid(g[i]).open;
         }
 #pragma unroll
         for (int i = 0; i < T::E; ++i) x[i] = fmaf(GATE != kNoGate ? sc[i] * g[i] : sc[i], fmaf((y[i] - m) * r, wa[i], ba[i]), x[i]);
@@ -221,7 +229,7 @@ template <typename T, int GATE, int FROM> __global__ __launch_bounds__(kRowThrea
     for (int64_t r0 = (int64_t)blockIdx.x * T::R; r0 < a.n; r0 += step) {
         const int left = rows_left(a.n, r0, T::R);
         const bool on = l.row < left;
-        float d[T::E], n[T::E], x[T::E], y[T::E], g[T::E], s[4];
+        float d[T::E], n[T::E], x[T::E], y[T::E], g[T::E], shut[T::E], s[4];
         take(rn, n);
         take(rd, d);
         take(rs, s);
@@ -230,12 +238,19 @@ template <typename T, int GATE, int FROM> __global__ __launch_bounds__(kRowThrea
         if constexpr (GATE == kFullGate) {
             ig.get(on, g);
 #pragma unroll
-            for (int i = 0; i < T::E; ++i) g[i] = sigmoid(g[i]);
+            for (int i = 0; i < T::E; ++i) {
+                const Sigmoid one = sigmoid(g[i]);
+                g[i] = one.open;
+                shut[i] = one.shut;
+            }
         }
         if constexpr (GATE == kRowGate) {
-            const float one = sigmoid(of_bits(rone));
+            const Sigmoid one = sigmoid(of_bits(rone));
 #pragma unroll
-            for (int i = 0; i < T::E; ++i) g[i] = one;
+            for (int i = 0; i < T::E; ++i) {
+                g[i] = one.open;
+                shut[i] = one.shut;
+            }
         }
         load(r0 + step);
 #pragma unroll
@@ -257,7 +272,7 @@ template <typename T, int GATE, int FROM> __global__ __launch_bounds__(kRowThrea
             du[i] = d[i] * sc[i];
             if constexpr (GATE != kNoGate) {
                 du[i] *= g[i];
-                dg[i] = du[i] * u * (1.0f - g[i]);
+                dg[i] = du[i] * u * shut[i];
                 sum[2][i] = fmaf(d[i] * g[i], u, sum[2][i]);
             } else {
                 sum[2][i] = fmaf(d[i], u, sum[2][i]);
