@@ -30,6 +30,17 @@ template <typename T> __device__ __forceinline__ void vec_load(const float* p, c
         }
 }
 
+// A row's mean where this lane has columns, zero past the width: what is there stays zero when the mean is taken off, and adds nothing to a row's
+// sums.  (A mean times a reciprocal deviation may be past the range of fp32: in rows of one value.)
+template <typename T> struct Mean {
+    float of[T::V];
+    __device__ __forceinline__ Mean(float m, const RowLane<T>& l, int D) {
+#pragma unroll
+        for (int v = 0; v < T::V; ++v) of[v] = l.col(v) < D ? m : 0.f;
+    }
+    __device__ __forceinline__ float operator[](int i) const { return of[i / T::W]; }
+};
+
 // mean (0 for RMS) and reciprocal deviation of a row; elements past the width are zeros
 template <typename T>
 __device__ __forceinline__ void row_stats(const float (&x)[T::E], const RowLane<T>& l, RowSums& sums, int D, bool layer, float inv, float eps, float& m,
@@ -41,9 +52,10 @@ __device__ __forceinline__ void row_stats(const float (&x)[T::E], const RowLane<
         for (int i = 0; i < T::E; ++i) s += x[i];
         m = sums.sum<T>(s) * inv;
         s = 0.f;
+        const Mean<T> mean(m, l, D);
 #pragma unroll
         for (int i = 0; i < T::E; ++i) {
-            const float c = l.col(i / T::W) < D ? x[i] - m : 0.f;
+            const float c = x[i] - mean[i];
             s = fmaf(c, c, s);
         }
     } else {
@@ -129,8 +141,9 @@ template <typename T, int GATE, bool CKPT> __global__ __launch_bounds__(kRowThre
 #pragma unroll
             for (int i = 0; i < T::E; ++i) g[i] = sigmoid(g[i]).open;
         }
+        const Mean<T> my(m, l, D);
 #pragma unroll
-        for (int i = 0; i < T::E; ++i) x[i] = fmaf(GATE != kNoGate ? sc[i] * g[i] : sc[i], fmaf((y[i] - m) * r, wa[i], ba[i]), x[i]);
+        for (int i = 0; i < T::E; ++i) x[i] = fmaf(GATE != kNoGate ? sc[i] * g[i] : sc[i], fmaf((y[i] - my[i]) * r, wa[i], ba[i]), x[i]);
         store_rows<T>(rows_view(a.X_out, r0, left, 4 * D), l, x);
         if constexpr (CKPT) store_codes<T>(rows_view(a.saved.x.q, r0, left, D), scales_view(a.saved.x.scale, r0, a.n, groups), l, on, x);
         row_stats<T>(x, l, sums, D, layer, inv, eps, m, r);
@@ -145,7 +158,8 @@ template <typename T, int GATE, bool CKPT> __global__ __launch_bounds__(kRowThre
 
 // gradient of a norm's input from that of its result: r * (g - [layer] mean(g) - xh * mean(g * xh)), in place of g
 template <typename T>
-__device__ __forceinline__ void norm_back(float (&g)[T::E], const float (&xh)[T::E], RowSums& sums, float r, bool layer, float inv) {
+__device__ __forceinline__ void norm_back(float (&g)[T::E], const float (&xh)[T::E], const RowLane<T>& l, RowSums& sums, float r, int D, bool layer,
+                                          float inv) {
     float s = 0.f, sx = 0.f;
 #pragma unroll
     for (int i = 0; i < T::E; ++i) sx = fmaf(g[i], xh[i], sx);
@@ -158,8 +172,9 @@ __device__ __forceinline__ void norm_back(float (&g)[T::E], const float (&xh)[T:
         sx = sums.sum<T>(sx);
     }
     sx *= inv;
+    const Mean<T> mean(s, l, D);
 #pragma unroll
-    for (int i = 0; i < T::E; ++i) g[i] = r * fmaf(-xh[i], sx, g[i] - s);
+    for (int i = 0; i < T::E; ++i) g[i] = r * fmaf(-xh[i], sx, g[i] - mean[i]);
 }
 
 // A tensor's rows of which nothing, fp32 elements or codes are there
@@ -185,8 +200,8 @@ template <typename T, int FROM> struct Incoming {
     }
 };
 
-// Columns past the width hold whatever the arithmetic makes of zeros: parameters are zeros there, so they add nothing to a row's sums, and
-// they are neither stored nor part of the sums over rows.  Rows past the end are zeros throughout, their statistics among them; so is all that
+// Columns past the width are zeros throughout, but for a gate's half: they add nothing to a row's sums, and they are neither stored nor part of the
+// sums over rows.  Rows past the end are zeros throughout, their statistics among them; so is all that
 // belongs to a part that is left out.
 template <typename T, int GATE, int FROM> __global__ __launch_bounds__(kRowThreads) void block_bwd_kernel(BlockBwd a) {
     __shared__ float sh[2][kRowThreads / kWave][2];
@@ -253,21 +268,22 @@ template <typename T, int GATE, int FROM> __global__ __launch_bounds__(kRowThrea
             }
         }
         load(r0 + step);
+        const Mean<T> mx(s[0], l, D), my(s[2], l, D);
 #pragma unroll
         for (int i = 0; i < T::E; ++i) {
-            x[i] = (x[i] - s[0]) * s[1];
+            x[i] = (x[i] - mx[i]) * s[1];
             sum[3][i] = fmaf(n[i], x[i], sum[3][i]);
             sum[4][i] += n[i];
             n[i] *= wb[i];
         }
-        norm_back<T>(n, x, sums, s[1], layer, inv);
+        norm_back<T>(n, x, l, sums, s[1], D, layer, inv);
 #pragma unroll
         for (int i = 0; i < T::E; ++i) d[i] += n[i];
         store_rows<T>(rows_view(a.grads.dX, r0, left, 4 * D), l, d);
         float dg[T::E], du[T::E];
 #pragma unroll
         for (int i = 0; i < T::E; ++i) {
-            y[i] = (y[i] - s[2]) * s[3];
+            y[i] = (y[i] - my[i]) * s[3];
             const float u = fmaf(y[i], wa[i], ba[i]);
             du[i] = d[i] * sc[i];
             if constexpr (GATE != kNoGate) {
@@ -289,7 +305,7 @@ template <typename T, int GATE, int FROM> __global__ __launch_bounds__(kRowThrea
             row = sums.sum<T>(row);
             __builtin_amdgcn_raw_buffer_store_b32(bits(row), rows_view(a.grads.dG, r0, left, 4), l.t == 0 ? l.row * 4 : kOutside, 0, 0);
         }
-        norm_back<T>(du, y, sums, s[3], layer, inv);
+        norm_back<T>(du, y, l, sums, s[3], D, layer, inv);
         store_rows<T>(rows_view(a.grads.dY, r0, left, 4 * D), l, du);
     }
     float* const part = a.part + (size_t)blockIdx.x * kSums * D;
