@@ -224,7 +224,8 @@ int dr_block_fwd(const dr_block* block, int64_t n, int32_t D, const float* X, co
  * dw_before, db_before [D] are overwritten; NULL = not wanted.  dX, dY and a dG of D columns may be dX_out, dN or a given Y, X_out or G (of D
  * columns) themselves, each another one; a dG of one column may be its G.
  * workspace: at least dr_block_bwd_workspace_bytes() bytes, 256-byte aligned, contents undefined before and after; it
- * belongs to one call at a time.  Sums over rows have a fixed order: a pass is reproducible bit for bit.
+ * belongs to one call at a time.  Sums over rows are in fp32 over sixteen rows and in 64 bits beyond (a workgroup's sum is rounded to fp32 once), in
+ * a fixed order: a pass is reproducible bit for bit.
  */
 typedef struct dr_block_grads {
     float *dX, *dY, *dG;

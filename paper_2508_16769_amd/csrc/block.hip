@@ -18,6 +18,10 @@
 namespace drc {
 
 constexpr int kSums = 5;                       // dw_after, db_after, dscale, dw_before, db_before
+// Rows that a lane adds up in fp32; those sums are added in 64 bits, so that what is lost does not grow with the rows: 16 additions, and the roundings of
+// a workgroup's sum and of the result.  A thread's wide sums are in LDS and its own: additions there without a result to wait for (1.2 M x 128 from
+// checkpoints 495 us; read, added and written back 504, every 32 rows 503).
+constexpr int kWiden = 16;
 
 // a parameter vector's elements of this lane; zeros past the width
 template <typename T> __device__ __forceinline__ void vec_load(const float* p, const RowLane<T>& l, int D, float none, float (&x)[T::E]) {
@@ -205,7 +209,7 @@ template <typename T, int FROM> struct Incoming {
 // belongs to a part that is left out.
 template <typename T, int GATE, int FROM> __global__ __launch_bounds__(kRowThreads) void block_bwd_kernel(BlockBwd a) {
     __shared__ float sh[2][kRowThreads / kWave][2];
-    __shared__ float all[T::R][T::LPR * T::E];
+    __shared__ double all[kSums * T::E][kRowThreads];         // every thread's own sums
     RowSums sums{sh, 0};
     const int D = a.D, groups = act_groups(D);
     const RowLane<T> l(D);
@@ -222,6 +226,20 @@ template <typename T, int GATE, int FROM> __global__ __launch_bounds__(kRowThrea
     for (int p = 0; p < kSums; ++p)
 #pragma unroll
         for (int i = 0; i < T::E; ++i) sum[p][i] = 0.f;
+    int since = 0;
+    bool wide = false;                                         // there is something in `all`
+    const auto widen = [&]() {
+#pragma unroll
+        for (int p = 0; p < kSums; ++p)
+#pragma unroll
+            for (int i = 0; i < T::E; ++i) {
+                if (wide) __hip_atomic_fetch_add(&all[T::E * p + i][threadIdx.x], (double)sum[p][i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                else all[T::E * p + i][threadIdx.x] = (double)sum[p][i];
+                sum[p][i] = 0.f;
+            }
+        wide = true;
+        since = 0;
+    };
     const int64_t step = (int64_t)gridDim.x * T::R;
     // what the next rows bring
     uint32_t rd[T::E], rn[T::E], rs[4], rone;
@@ -307,21 +325,17 @@ template <typename T, int GATE, int FROM> __global__ __launch_bounds__(kRowThrea
         }
         norm_back<T>(du, y, l, sums, s[3], D, layer, inv);
         store_rows<T>(rows_view(a.grads.dY, r0, left, 4 * D), l, du);
+        if (++since == kWiden) widen();
     }
+    widen();
+    __syncthreads();
     float* const part = a.part + (size_t)blockIdx.x * kSums * D;
-    for (int p = 0; p < kSums; ++p) {
-        __syncthreads();
+    for (int i = threadIdx.x; i < kSums * T::E * T::LPR; i += kRowThreads) {
+        const int lane = i % T::LPR, e = i / T::LPR % T::E, p = i / (T::LPR * T::E), c = T::W * (lane + T::LPR * (e / T::W)) + e % T::W;
+        double s = 0.0;
 #pragma unroll
-        for (int v = 0; v < T::V; ++v)
-#pragma unroll
-            for (int j = 0; j < T::W; ++j) all[l.row][l.col(v) + j] = sum[p][T::W * v + j];
-        __syncthreads();
-        for (int c = threadIdx.x; c < D; c += kRowThreads) {
-            float s = 0.f;
-#pragma unroll
-            for (int k = 0; k < T::R; ++k) s += all[k][c];
-            part[(size_t)p * D + c] = s;
-        }
+        for (int k = 0; k < T::R; ++k) s += all[T::E * p + e][T::LPR * k + lane];
+        if (c < D) part[(size_t)p * D + c] = (float)s;
     }
 }
 
