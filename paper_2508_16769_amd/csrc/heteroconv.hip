@@ -655,7 +655,7 @@ static int backward_pass(const LayerBwd* g, int n, const dr_heteroconv_weights* 
     }
     // The weight gradients come first: what the projections write is then gathered right away.
     if (!alone) {
-        if (!need_dx) return launch_wgrads(wj, 2 * n, D, s);
+        if (!need_dx) return opt.saved8 ? launch_wgrads8(w8, 2, D, s) : launch_wgrads(wj, 2 * n, D, s);
         PendingSums sums{};
         if (opt.saved8) DRC_TRY(launch_dense_bwd8(w8, pj, *W, D, g[0].c->wg_sums, &sums, s));
         else DRC_TRY(launch_dense_bwd(wj, pj, n, *W, D, g[0].c->wg_sums, &sums, s));
@@ -727,6 +727,7 @@ template <typename F> static int in_scratch(dr_heteroconv* const* c, int n, hipS
 
 int drc::heteroconv_backward(const LayerBwd* g, int n, const dr_heteroconv_weights* W, hipStream_t s, BackwardOptions opt) {
     DRC_REQUIRE(n >= 1 && n <= kMaxGraphs, "heteroconv_bwd: %d graphs in one pass", n);
+    DRC_REQUIRE(!opt.saved8 || n == 1, "heteroconv_bwd: checkpoints of %d graphs in one pass", n);
     dr_heteroconv* c[kMaxGraphs];
     for (int i = 0; i < n; ++i) c[i] = g[i].c;
     return in_scratch(c, n, s, [&] { return backward_pass(g, n, W, s, opt); });
