@@ -438,11 +438,12 @@ int heteroconv_set_overlap(dr_heteroconv* ctx, int mode);
 
 /*
  * Measurement aid (not part of the method): per-kernel device time of the layer's launches.
- * heteroconv_profile(ctx, 1) makes every later heteroconv_fwd / heteroconv_bwd give every relation
+ * heteroconv_profile(ctx, 1) makes every later heteroconv_fwd / heteroconv_bwd (the 8-bit ones among them) give every relation
  * launches of its own (as DR_OVERLAP_OFF) and bracket each with HIP events on the caller's stream; heteroconv_profile(ctx, 0)
  * stops that.  heteroconv_kernel_times synchronises the device, adds up the elapsed time per kernel id since
  * the previous call into ms_sum[n] / launches[n] (host arrays, n >= heteroconv_num_kernels()) and forgets the
- * recorded launches.  heteroconv_kernel_name(id) names a kernel id ("dr_spmm_fwd.near", ...).
+ * recorded launches.  heteroconv_kernel_name(id) names a kernel id ("dr_spmm_fwd.near", ...); packing the messages of
+ * heteroconv_fwd_act8 is one ("dr_act8_pack.messages").
  * With profiling on, the calls create HIP events on demand (host-side allocation).
  */
 int heteroconv_profile(dr_heteroconv* ctx, int enable);

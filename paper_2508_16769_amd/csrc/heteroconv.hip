@@ -18,12 +18,13 @@ namespace {
 // kernel ids for the optional per-kernel timing (heteroconv_profile / heteroconv_kernel_times)
 enum KernelId {
     kTopkCell, kTopkNet, kFwdNear, kFwdPins, kFwdPinned, kProjCell, kProjPins,
-    kWgCell, kWgPins, kDhCell, kDhPins, kBwdNear, kBwdNearPins, kBwdPins, kBwdPinned, kNumKernels
+    kWgCell, kWgPins, kDhCell, kDhPins, kBwdNear, kBwdNearPins, kBwdPins, kBwdPinned, kPack8, kNumKernels
 };
 const char* const kKernelNames[kNumKernels] = {
     "dr_topk.cell", "dr_topk.net", "dr_spmm_fwd.near", "dr_spmm_fwd.pins", "dr_spmm_fwd.pinned",
     "proj.cell+merge", "proj.pins", "wgrad.cell", "wgrad.pins", "dproj.cell", "dproj.pins",
-    "dr_spmm_bwd.near", "dr_spmm_bwd.near+pins+dX", "dr_spmm_bwd.pins+dX", "dr_spmm_bwd.pinned+dX"};
+    "dr_spmm_bwd.near", "dr_spmm_bwd.near+pins+dX", "dr_spmm_bwd.pins+dX", "dr_spmm_bwd.pinned+dX",
+    "dr_act8_pack.messages"};
 struct TimedLaunch { int id; hipEvent_t start, stop; bool start_shared; };   // start_shared: start is the previous launch's stop
 }  // namespace
 
@@ -765,6 +766,7 @@ int heteroconv_fwd_act8(dr_heteroconv* c, const float* X_cell, const float* X_ne
     return in_scratch(&c, 1, s, [&]() -> int {
         DRC_TRY(heteroconv_forward(&g, 1, W, s, ForwardOptions{}));
         const Act8Pack jobs[3] = {{full.H_near, c->Nc, S->H_near}, {full.H_pinned, c->Nc, S->H_pinned}, {full.H_pins, c->Nn, S->H_pins}};
+        ScopedTiming tm(c, kPack8, s);
         return launch_act8_packs(jobs, 3, c->D, s);
     });
 }
