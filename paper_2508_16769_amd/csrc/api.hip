@@ -235,6 +235,7 @@ int dr_block_fwd(const dr_block* block, int64_t n, int32_t D, const float* X, co
     DRC_REQUIRE(N != nullptr || S.stats_before == nullptr, "dr_block_fwd: statistics of a norm in front without N");
     DRC_REQUIRE(S.g.q == nullptr || block->gate_cols == D, "dr_block_fwd: a checkpoint of G needs gate_cols = D");
     DRC_REQUIRE(X_out == nullptr || X_out != N, "dr_block_fwd: X_out and N are the same");
+    DRC_REQUIRE(G == nullptr || block->gate_cols == D || (G != X_out && G != N), "dr_block_fwd: a gate of one column is no room for X_out or N");
     DRC_REQUIRE(aligned(X, 4) && aligned(Y, 4) && aligned(G, 4) && aligned(X_out, 4) && aligned(N, 4) && aligned(S.stats_after, 4) &&
                     aligned(S.stats_before, 4),
                 "dr_block_fwd: misaligned pointer");
@@ -270,6 +271,10 @@ int dr_block_bwd(const dr_block* block, int64_t n, int32_t D, const float* dX_ou
         DRC_REQUIRE(S.g.q == nullptr || block->gate_cols == D, "dr_block_bwd: a checkpoint of G needs gate_cols = D");
         DRC_REQUIRE(after || (!g.dY && !g.dG && !g.dw_after && !g.db_after && !g.dscale), "dr_block_bwd: gradients behind the layer without Y");
         DRC_REQUIRE(gated || !g.dG, "dr_block_bwd: dG without G");
+        const bool row_gate = gated && block->gate_cols != D;
+        DRC_REQUIRE(!row_gate || (G != g.dX && G != g.dY), "dr_block_bwd: a gate of one column is no room for dX or dY");
+        DRC_REQUIRE(!row_gate || !g.dG || (g.dG != dX_out && g.dG != dN && g.dG != X_out && g.dG != Y),
+                    "dr_block_bwd: a dG of one column takes no other tensor's place than G's");
         if (S.x.q) DRC_TRY(check_act8(&S.x, "dr_block_bwd", "x"));
         if (S.y.q) DRC_TRY(check_act8(&S.y, "dr_block_bwd", "y"));
         if (S.g.q) DRC_TRY(check_act8(&S.g, "dr_block_bwd", "g"));
