@@ -176,7 +176,8 @@ int dr_act8_unpack(const dr_act8* in, int64_t n, int32_t D, float* X, void* stre
 /*
  * Weight gradient of a dense projection Z = A W whose input A[n,D] was kept as a checkpoint:
  *     dW[D,F] (=|+=) A^T dZ,          A the values the checkpoint stands for, dZ[n,F] in fp32.
- * accumulate == 0 overwrites dW.  Products are exact to 2^-24 and summed in fp32 and fp64, in a fixed order.
+ * accumulate == 0 overwrites dW.  Products are exact to 2^-24 (what lies below 2^-133 in a dZ below 2^-110 is left out) and
+ * summed in fp32 and fp64, in a fixed order.
  * 1 <= D, F <= DR_MAX_D.  workspace: at least dr_act8_wgrad_workspace_bytes() bytes, 256-byte aligned, contents undefined
  * before and after; it belongs to one call at a time.
  */

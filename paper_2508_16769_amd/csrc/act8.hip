@@ -99,7 +99,8 @@ int launch_act8_unpack(const dr_act8& in, int64_t n, int D, float* X, hipStream_
 // dW[D,F] = A^T dZ, the contraction running over the rows.
 //
 // Arithmetic.  What a code stands for, q * 2^s, is a bf16 number exactly; dZ is cut into three bf16 numbers, x = x1 + x2 + x3,
-// by taking the upper half of x, of x - x1 and of x - x1 - x2: 3 x 8 significant bits hold all 24.  Three exact bf16 products per
+// by taking the upper half of x, of x - x1 and of x - x1 - x2: 3 x 8 significant bits hold all 24 from 2^-110 upwards; below, bf16's steps end
+// at 2^-133 and what is smaller is left out.  Three exact bf16 products per
 // term then are the fp32 product (a projection whose input is held in fp32 needs six).  Leading products and small ones have
 // accumulators of their own, which start from zero every kFlush chunks and are added to the running sum with one rounding:
 // inside the matrix unit what lies below the running sum is cut off, always downwards, which over many rows adds up.
