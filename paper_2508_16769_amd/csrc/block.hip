@@ -374,8 +374,9 @@ __global__ __launch_bounds__(kWave* kSumWaves) void block_sums_kernel(const floa
 // read a column at a time, and take three: 200 000 x 77, 512 / 768 / 1024: forward 58 / 55 / 58, with checkpoints 89 / 83 / 85, backward from
 // checkpoints 81 / 73 / 78; 500 000 x 45 123 / 94 / 88, 151 / 140 / 138, 157 / 129 / 125; 20 000 x 999 61 / 64 / 66, 86 / 83 / 84, 86 / 84 / 87.
 template <typename T> constexpr int kBlockWgs = T::W == 4 ? 512 : 768;
-// Forward with a gate per element and checkpoints, ten tensors at once: one per compute unit, 256 / 512 workgroups, 500 000 x 128 290 / 314,
-// 1 M x 64 287 / 313; not where the caches hold them (60 000 x 128 41 / 37).
+// Forward with a gate per element and checkpoints, ten tensors at once: one per compute unit from 2^25 elements on, where every lane has columns.  256 / 512
+// workgroups, us: 12 M elements 61 / 57 (D = 64, 128 and 256), 25 M 116 / 117, 29 M 135 / 136, 34 M 153 / 153, 40 M 182 / 187, 64 M 291 / 320; with a
+// quarter of the lanes idle (D = 96) 34 M 186 / 167, 64 M 350 / 325.
 constexpr int64_t kManyTensorsFrom = int64_t(1) << 25;     // elements
 static bool vector_rows(int D, std::initializer_list<const void*> f32, std::initializer_list<const void*> q) {
     bool v = D % 4 == 0;
@@ -396,7 +397,7 @@ int launch_block_fwd(const BlockFwd& a, hipStream_t s) {
     return with_row_tile(a.D, vector, [&](auto tile) -> int {
         using T = decltype(tile);
         const int64_t rows = ckpt ? (a.n + 7) / 8 * 8 : a.n, blocks = (rows + T::R - 1) / T::R;
-        const bool many = T::W == 4 && ckpt && a.b.gate_cols == a.D && a.n * a.D >= kManyTensorsFrom;
+        const bool many = T::W == 4 && a.D == T::W * T::LPR && ckpt && a.b.gate_cols == a.D && a.n * a.D >= kManyTensorsFrom;
         const int64_t most = many ? kBlockWgs<T> / 2 : kBlockWgs<T>;
         const dim3 grid((unsigned)(blocks < most ? blocks : most));
         auto go = [&](auto gate) {
