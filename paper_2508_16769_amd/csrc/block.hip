@@ -55,6 +55,7 @@ __device__ __forceinline__ void row_stats(const float (&x)[T::E], const RowLane<
 #pragma unroll
         for (int i = 0; i < T::E; ++i) s += x[i];
         m = sums.sum<T>(s) * inv;
+        asm volatile("" : "+v"(m));                // the mean that is saved: not the exact product inside the subtractions below
         s = 0.f;
         const Mean<T> mean(m, l, D);
 #pragma unroll
