@@ -35,12 +35,13 @@ template <typename T> __device__ __forceinline__ void vec_load(const float* p, c
 }
 
 // A row's mean where this lane has columns, zero past the width: what is there stays zero when the mean is taken off, and adds nothing to a row's
-// sums.  (A mean times a reciprocal deviation may be past the range of fp32: in rows of one value.)
+// sums.  (A mean times a reciprocal deviation may be past the range of fp32: in rows of one value.)  Only the last of a lane's loads can be past the
+// width, tiles are the narrowest: asked of all of them, 500 000 x 45 backward takes 124.5 us instead of 121.6.
 template <typename T> struct Mean {
     float of[T::V];
     __device__ __forceinline__ Mean(float m, const RowLane<T>& l, int D) {
 #pragma unroll
-        for (int v = 0; v < T::V; ++v) of[v] = l.col(v) < D ? m : 0.f;
+        for (int v = 0; v < T::V; ++v) of[v] = v + 1 < T::V || l.col(v) < D ? m : 0.f;
     }
     __device__ __forceinline__ float operator[](int i) const { return of[i / T::W]; }
 };
