@@ -192,8 +192,9 @@ int dr_act8_wgrad(const dr_act8* A, int64_t n, int32_t D, const float* dZ, int32
  *     N     = norm(X_out) * w_before + b_before                             (the next layer's input)
  *     norm(x) = x * r,  r = 1 / sqrt(mean(x^2) + eps)                 DR_ROWNORM_RMS
  *     norm(x) = (x - m) * r,  m = mean(x), r = 1 / sqrt(mean((x - m)^2) + eps)      DR_ROWNORM_LAYER
- * Means are over the D entries of a row, in fp32: a row whose squares overflow has r = 0.  G has gate_cols columns: D (a gate per element), 1 (one per row) or 0 (no gate,
- * G NULL).  w_*, b_* and scale are [D]; NULL stands for ones, zeros and ones.
+ * Means are over the D entries of a row, in fp32: a row whose squares overflow has r = 0, one whose sum does (DR_ROWNORM_LAYER) has
+ * not-a-numbers.  G has gate_cols columns: D (a gate per element), 1 (one per row) or 0 (no gate, G NULL).  w_*, b_* and scale are [D];
+ * NULL stands for ones, zeros and ones.
  * Y NULL: only the norm in front, N of X (X_out, G, y and g are NULL then, and saved.x is the checkpoint of X).
  * N NULL: only the part behind the layer.  One of Y and N is given.
  */

@@ -7,8 +7,8 @@
 //   t = d * scale;  du = t * sig;  dG = t * u * sig * (1 - sig);  dscale = sum d * sig * u
 //   g = du * w_after;  dY = r2 * (g - [layer] mean(g) - yh * mean(g * yh))
 //   dw_after = sum du * yh, db_after = sum du, dw_before = sum dN * xh, db_before = sum dN          (sums over rows)
-// A row stays in registers from its load to its stores; what bounds both passes is memory: forward of 1.2 M x 128 443 us (2.46 GB, 5.5 TB/s), backward
-// from checkpoints 496 (2.77 GB, 5.6 TB/s); with a gate per element and three checkpoints 500 000 x 128 forward 285 (1.48 GB, 5.2 TB/s).  The sums over rows
+// A row stays in registers from its load to its stores; what bounds both passes is memory: forward of 1.2 M x 128 443 to 449 us by card (2.47 GB, 5.5 TB/s), backward
+// from checkpoints with a gate per row 493 to 505, its sums included (2.79 GB, 5.6 TB/s); with a gate per element and three checkpoints 500 000 x 128 forward 285 to 290 (1.48 GB, 5.2 TB/s).  The sums over rows
 // of the backward pass are a second launch, 2.5 to 5 us.
 #include "act8.h"
 
@@ -90,7 +90,7 @@ __device__ __forceinline__ Buf stats_view(const float* p, int64_t r0, int left, 
 
 // The loops below have no memory access under a condition: what is absent has an empty view.  The compiler then knows how many loads and stores
 // are outstanding wherever it has to wait for some of them; with branches around loads and stores every row waited for the loads of
-// the next one (1.2 M x 128 backward from checkpoints, two workgroups per compute unit: 627 us, now 496).
+// the next one (1.2 M x 128 backward from checkpoints, two workgroups per compute unit: 627 us, without them 496).
 // A row's loads do wait for the stores of the row before, and that is left as it is: with as many empty stores in front of the loop as it ends with
 // the compiler lets them pass, and workgroups then spread over more of memory's pages (forward 443 / 456, backward 496 / 540 us).
 enum Gate { kNoGate, kRowGate, kFullGate };
@@ -371,10 +371,10 @@ __global__ __launch_bounds__(kWave* kSumWaves) void block_sums_kernel(const floa
 }
 
 // Workgroups of a launch: few that walk many rows.  Two per compute unit draw 5.6 TB/s from memory, more of them drift apart and find its
-// pages closed: 1.2 M x 128, 512 / 768 / 1024 / 2048 workgroups, us: forward 443 / 486 / 530 / 580, backward from checkpoints 496 / 552 / 590 /
-// 610; 60 000 x 128 24.4 / 25.4 / 25.7 / 26.0 and 32.8 / 34.5 / 35.5 / 39.4; 256 leave a SIMD one wavefront (528 and 605).  Rows of any width are
-// read a column at a time, and take three: 200 000 x 77, 512 / 768 / 1024: forward 58 / 55 / 58, with checkpoints 89 / 83 / 85, backward from
-// checkpoints 81 / 73 / 78; 500 000 x 45 123 / 94 / 88, 151 / 140 / 138, 157 / 129 / 125; 20 000 x 999 61 / 64 / 66, 86 / 83 / 84, 86 / 84 / 87.
+// pages closed: 1.2 M x 128, 512 / 768 / 1024 workgroups, us: forward 449 / 498 / 537, with two checkpoints 565 / 581 / 638, backward from checkpoints 506 / 562 /
+// 594, from tensors 697 / 725 / 827; 60 000 x 128 19.7 / 20.0 / 20.5, 23.2 / 23.1 / 23.5, 28.0 / 29.0 / 30.4, 33.1 / 34.4 / 36.2.  Rows of any width are
+// read a column at a time, and take three: 200 000 x 77 38 / 39 / 40, 87 / 82 / 83, 80 / 73 / 77, 75 / 79 / 84; 500 000 x 45 124 / 93 / 85, 150 / 139 / 138,
+// 153 / 127 / 122, 139 / 122 / 126; 20 000 x 999 59 / 60 / 62, 85 / 80 / 81, 86 / 82 / 97, 96 / 104 / 114.
 template <typename T> constexpr int kBlockWgs = T::W == 4 ? 512 : 768;
 // Forward with a gate per element and checkpoints, ten tensors at once: one per compute unit from 2^25 elements on, where every lane has columns.  256 / 512
 // workgroups, us: 12 M elements 61 / 57 (D = 64, 128 and 256), 25 M 116 / 117, 29 M 135 / 136, 34 M 153 / 153, 40 M 182 / 187, 64 M 291 / 320; with a

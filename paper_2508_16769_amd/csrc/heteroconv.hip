@@ -734,8 +734,8 @@ int drc::heteroconv_backward(const LayerBwd* g, int n, const dr_heteroconv_weigh
     return in_scratch(c, n, s, [&] { return backward_pass(g, n, W, s, opt); });
 }
 
-// What the 8-bit messages cost and bring (saved bytes, forward, backward; plain / 8 bits): 1.2 M cells, D = 128, k = 32 2 142 / 946 MiB, 2 281 / 2 681 us,
-// 3 567 / 3 427; 60 000, 64, 16 52 / 23 MiB, 76 / 83, 104 / 102; 2 048, 64, 16 22.0 / 24.7, 27.7 / 27.6.  The forward pass packs in a launch of its own
+// What the 8-bit messages cost and bring (saved bytes, forward, backward; plain / 8 bits): 1.2 M cells, D = 128, k = 32 2 142 / 946 MiB, 2 262 / 2 646 us,
+// 3 426 / 3 347; 250 000 cells 441 / 195 MiB, 500 / 549, 710 / 674; 60 000, 64, 16 52 / 23 MiB, 76 / 83, 103 / 103; 2 048, 64, 16 22.0 / 24.7, 27.7 / 27.6.  The forward pass packs in a launch of its own
 // behind the projections (2.1 GB at 5.6 TB/s in the first case); weight gradients read a byte instead of four and take three bf16 products per
 // message instead of six.
 // ---- messages kept in 8 bits ----------------------------------------------------------------------------------------------------
