@@ -343,7 +343,10 @@ def dr_block_bwd(dX_out: Optional[torch.Tensor], dN: Optional[torch.Tensor], X_o
                  w_before=None, b_before=None, stats_after=None, stats_before=None, x8=None, y8=None, g8=None, dX=None, dY=None,
                  dG=None, dw_after=None, db_after=None, dscale=None, dw_before=None, db_before=None, workspace=None, stream=None) -> None:
     """x8, y8, g8: checkpoints that stand in for X_out, Y and G where those are None."""
-    n, D = (dX_out if dX_out is not None else dN).shape
+    some = dX_out if dX_out is not None else dN
+    if some is None:                                          # the library refuses the call, whatever sizes it hears of
+        some = next((t for t in (X_out, Y, *(c[0] for c in (x8, y8) if c)) if t is not None), None)
+    n, D = (0, 0) if some is None else some.shape
     b = dr_block(norm, _gate_cols(G, g8), eps, _address(w_after), _address(b_after), _address(scale), _address(w_before), _address(b_before))
     s = dr_block_saved(_address(stats_after), _address(stats_before), _act8(x8), _act8(y8), _act8(g8))
     g = dr_block_grads(_address(dX), _address(dY), _address(dG), _address(dw_after), _address(db_after), _address(dscale),
